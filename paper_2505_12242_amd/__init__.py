@@ -3,8 +3,10 @@
 Per bf16 weight gradient: per-input-channel squared norms, top-k channel
 selection, in-place Adam on the selected channels' fp32 states with bf16
 write-back, and S-step accumulation of the unselected channels in a packed
-fp32 buffer handed over as a dense matrix.  All of it runs in the HIP
-kernels of libzf.so (C ABI in include/zf.h); this package only binds it.
+fp32 buffer handed over as a dense matrix.  Around it, the layer the weights belong
+to: RMS norm, 8-bit quantiser and matrix product, and AdamW over the many
+tensors that are not split by channel (layer.py).  All of it runs in the HIP
+kernels of libzf.so (C ABI in include/); this package only binds it.
 """
 
 from ._lib import (  # noqa: F401
@@ -41,5 +43,18 @@ from ._lib import (  # noqa: F401
     unpack,
     update_fused,
     update_fused_handover,
+)
+from .layer import (  # noqa: F401
+    AdamWBuffers,
+    AdamWPlan,
+    Fp8,
+    RmsNorm,
+    alloc_fp8,
+    matmul_fp8,
+    matmul_fp8_workspace_bytes,
+    quantize_fp8,
+    rmsnorm,
+    rmsnorm_backward,
+    rmsnorm_backward_workspace_bytes,
 )
 from .runner import SelectiveUpdateRunner, StepKind, schedule  # noqa: F401

@@ -66,7 +66,18 @@ class ZfZenTotals(ctypes.Structure):
                 ("trigger", c_i32), ("pad", c_i32)]
 
 
-# (name, restype, argtypes) of every exported entry point of include/zf.h.
+class ZfFp8(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("ld_data", c_i64), ("scale", c_vp), ("ld_scale", c_i64),
+                ("group", c_i32)]
+
+
+class ZfAdamwTensor(ctypes.Structure):
+    _fields_ = [("n", c_i64), ("grad", c_vp), ("grad_dtype", c_i32), ("master", c_vp),
+                ("weight", c_vp), ("exp_avg", c_vp), ("exp_avg_sq", c_vp),
+                ("exp_avg_scale", c_vp), ("exp_avg_sq_scale", c_vp)]
+
+
+# (name, restype, argtypes) of every exported entry point of include/*.h.
 SIGNATURES = [
     ("zf_status_string", ctypes.c_char_p, [ctypes.c_int]),
     ("zf_last_hip_error", ctypes.c_int, []),
@@ -135,6 +146,26 @@ SIGNATURES = [
      [c_vp, ctypes.POINTER(c_vp), c_i32, c_vp, c_vp]),
     ("zf_plan_update_zen_pending", ctypes.c_int,
      [c_vp, ctypes.POINTER(ZfAdamHparams), c_i64, c_i64, c_i64, c_flt, c_dbl, c_vp, c_vp]),
+    # include/zf_layer.h
+    ("zf_quantize_fp8", ctypes.c_int,
+     [c_vp, c_i32, c_i64, c_i64, c_i64, ctypes.POINTER(ZfFp8), ctypes.POINTER(ZfFp8), c_vp]),
+    ("zf_matmul_fp8_workspace_bytes", c_sz, [c_i64, c_i64, c_i64]),
+    ("zf_matmul_fp8", ctypes.c_int,
+     [ctypes.POINTER(ZfFp8), ctypes.POINTER(ZfFp8), c_i64, c_i64, c_i64, c_vp, c_i32, c_i64, c_vp,
+      c_sz, c_vp]),
+    ("zf_rmsnorm_forward", ctypes.c_int,
+     [c_vp, c_i64, c_vp, c_i64, c_i32, c_i64, c_i64, c_vp, c_i32, c_dbl, c_vp, c_i64, c_vp, c_i64,
+      ctypes.POINTER(ZfFp8), c_vp, c_vp]),
+    ("zf_rmsnorm_backward_workspace_bytes", c_sz, [c_i64, c_i64]),
+    ("zf_rmsnorm_backward", ctypes.c_int,
+     [c_vp, c_i64, c_vp, c_i64, c_i32, c_i64, c_i64, c_vp, c_i32, c_vp, c_vp, c_i64, c_vp, c_i64,
+      c_vp, c_vp, c_sz, c_vp]),
+    ("zf_adamw_plan_query", ctypes.c_int,
+     [ctypes.POINTER(ZfAdamwTensor), c_i32, ctypes.POINTER(c_sz)]),
+    ("zf_adamw_plan_create", ctypes.c_int,
+     [ctypes.POINTER(ZfAdamwTensor), c_i32, c_vp, c_sz, c_vp, ctypes.POINTER(c_vp)]),
+    ("zf_adamw_plan_destroy", None, [c_vp]),
+    ("zf_adamw_step", ctypes.c_int, [c_vp, ctypes.POINTER(ZfAdamHparams), c_i64, c_vp, c_vp]),
 ]
 
 

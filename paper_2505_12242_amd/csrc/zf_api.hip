@@ -38,22 +38,26 @@ AdamK adam_consts(const zf_adam_hparams& hp, int64_t step) {
   return c;
 }
 
+namespace {
+thread_local int g_last_hip_error = 0;
+}
+
+zf_status hip_fail(hipError_t e) {
+  g_last_hip_error = static_cast<int>(e);
+  return ZF_EHIP;
+}
+
 }  // namespace zf
 
 using zf::adam_consts;
+using zf::g_last_hip_error;
+using zf::hip_fail;
 using zf::hparams_ok;
 using zf::AdamK;
 using zf::DevMat;
 using zf::Table;
 
 namespace {
-
-thread_local int g_last_hip_error = 0;
-
-zf_status hip_fail(hipError_t e) {
-  g_last_hip_error = static_cast<int>(e);
-  return ZF_EHIP;
-}
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
