@@ -39,6 +39,7 @@ struct MatmulArgs {
   void* out;
   int64_t ld_out;
   int32_t out_f32;
+  int32_t share;  // steps of one share of the reduction, where it is split
 };
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t launch_matmul(const MatmulArgs& a, void* ws, hipStream_t s);

@@ -140,7 +140,7 @@ zf_status zf_matmul_fp8(const zf_fp8* a, const zf_fp8* b, int64_t m, int64_t n, 
   if (!disjoint({so, sw}, {sa.data, sa.scale, sb.data, sb.scale})) return ZF_EINVAL;
   if (m == 0 || n == 0) return ZF_OK;
   const zf::MatmulArgs args{operand(a), operand(b), m, n, k, out, ld_out,
-                            out_dtype == ZF_F32 ? 1 : 0};
+                            out_dtype == ZF_F32 ? 1 : 0, 0};
   return done(zf::launch_matmul(args, ws, as_stream(stream)));
 }
 

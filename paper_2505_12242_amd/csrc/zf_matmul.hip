@@ -3,6 +3,8 @@
 //
 // out[i][j] = sum over groups g of 2^(ca[i][g] + cb[j][g] - 254) * sum over
 // the group of a * b.
+#include <type_traits>
+
 #include "zf_layer.hpp"
 
 namespace zf {
@@ -10,157 +12,216 @@ namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+typedef __bf16 v4b __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int kBK = 128;  // reduction per step: one scale group
 
-// Tiles in units of 16 bytes: unit c of row r lies at this byte of the tile.
-// 16 consecutive rows reading one unit meet all 64 banks once.
+// A step's rows in LDS: 16-byte unit c (of 8) of row r lies at this byte.  16
+// consecutive rows reading one unit meet all 64 banks once.
 __device__ __forceinline__ int tile_off(int r, int c) {
   return r * kBK + ((c ^ ((r >> 1) & 7)) << 4);
 }
 
-// One 32 x 32 tile of the accumulator: += x y^T over 64 elements of the
-// reduction, of which a lane holds 32 of row lane % 32 (x: the tile's
-// registers, y: its lanes).  Two forms:
+// One phase of a wave: acc[i][j] += y_j x_i^T (32 x 32 tiles) over 64 elements of
+// the reduction, of which a lane holds 32 of row lane % 32 of each tile.  y's
+// rows run along the accumulator's registers, x's along its lanes.  Two forms:
 //   fast     the scaled 8-bit instruction.  It aligns 64 products to the
-//            largest of them and cuts what lies below 2^-13 of it (measured:
-//            1.3e-5 relative on normal data), far below the 2^-4 that e4m3
+//            largest of them and cuts what lies some 2^-13 below (measured:
+//            1.3e-5 relative on normal data), far less than the 2^-4 that e4m3
 //            itself cut and the 2^-9 of a bf16 result.
-//   precise  elements and scale to bf16 (exact), products and sums in fp32
+//   precise  elements times scale to bf16 (exact), products and sums in fp32
 //            (7e-9 relative), at 0.42 of the rate.  Taken for fp32 results.
-template <bool PRECISE>
-struct Operand;
-template <>
-struct Operand<false> {
-  v8i v;
-  __device__ __forceinline__ void set(u32x4 x, u32x4 y, int) {
-    v = v8i{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
-  }
-};
-template <>
-struct Operand<true> {
-  v8b v[4];
-  __device__ __forceinline__ void set(u32x4 x, u32x4 y, int scale) {
-    const float s = __uint_as_float(static_cast<uint32_t>(scale & 255) << 23);
+__device__ __forceinline__ void to_bf16(v8i x, int code, v8b (&out)[4]) {
+  const float s = __uint_as_float(static_cast<uint32_t>(code & 255) << 23);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t lo = q < 2 ? x[2 * q] : y[2 * q - 4], hi = q < 2 ? x[2 * q + 1] : y[2 * q - 3];
-      const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false);
-      const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true);
-      const v2b c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false);
-      const v2b d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true);
-      v[q] = v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  for (int q = 0; q < 4; ++q) {
+    const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * q], s, false);
+    const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * q], s, true);
+    const v2b c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * q + 1], s, false);
+    const v2b d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * q + 1], s, true);
+    out[q] = v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+}
+// Tiles [G TM TN / (TM + TN), (G + 1) TM TN / (TM + TN)) of a phase (row by row of
+// acc); cvt holds the precise form's y, and its x of the row at hand.
+template <int TM, int TN>
+struct Converted {
+  v8b x[4], y[TN][4];
+};
+template <bool PRECISE, int G, int TM, int TN>
+__device__ __forceinline__ void mma(const v8i (&x)[TM], const int (&cx)[TM], const v8i (&y)[TN],
+                                    const int (&cy)[TN], v16f (&acc)[TM][TN],
+                                    Converted<TM, TN>& cvt) {
+  if constexpr (PRECISE && G == 0)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) to_bf16(y[j], cy[j], cvt.y[j]);
+#pragma unroll
+  for (int t = G * TM * TN / (TM + TN); t < (G + 1) * TM * TN / (TM + TN); ++t) {
+    const int i = t / TN, j = t % TN;
+    if constexpr (!PRECISE) {
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y[j], x[i], acc[i][j], 0, 0, 0,
+                                                                  cy[j], 0, cx[i]);
+    } else {
+      if (j == 0) to_bf16(x[i], cx[i], cvt.x);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cvt.y[j][q], cvt.x[q], acc[i][j], 0, 0, 0);
     }
+#ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know the registers)
+    // (keeps the product from being moved behind what follows)
+    asm volatile("" : "+a"(acc[i][j]));
+#endif
   }
-};
-__device__ __forceinline__ v16f mma(const Operand<false>& x, int sx, const Operand<false>& y, int sy,
-                                    v16f acc) {
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x.v, y.v, acc, 0, 0, 0, sx, 0, sy);
 }
-__device__ __forceinline__ v16f mma(const Operand<true>& x, int, const Operand<true>& y, int,
-                                    v16f acc) {
+__device__ __forceinline__ v8i join(u32x4 x, u32x4 y) {
+  return v8i{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
+}
+
+// A 16-byte unit of an operand row with the bytes at and past `valid` cleared.
+__device__ __forceinline__ u32x4 clear_tail(u32x4 v, int valid) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v[q], y.v[q], acc, 0, 0, 0);
-  return acc;
+  for (int w = 0; w < 4; ++w) {
+    const int n = valid - 4 * w;  // bytes of this word that count
+    v[w] = n >= 4 ? v[w] : n <= 0 ? 0u : v[w] & ((1u << (8 * n)) - 1u);
+  }
+  return v;
 }
 
-// Stores 8 results of a row.
-__device__ __forceinline__ void put8(void* out, int64_t at, int64_t valid, bool f32,
-                                     const float (&v)[8]) {
-  if (f32) store8(static_cast<float*>(out) + at, valid, v);
-  else store8(static_cast<uint16_t*>(out) + at, valid, v);
+// Tile of block b in a grid of mt x nt.  Each XCD takes a contiguous range of
+// the order; within it 8 tile rows are walked together, so that the tiles an
+// XCD works on at once share rows of both operands in its L2.
+__device__ __forceinline__ void tile_of(uint32_t b, uint32_t mt, uint32_t nt, uint32_t& mi,
+                                        uint32_t& ni) {
+  constexpr uint32_t kRows = 8;
+  const uint32_t B = mt * nt, q = B / kXcds, r = B % kXcds, x = b % kXcds, i = b / kXcds;
+  const uint32_t id = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + i;
+  const uint32_t g = id / (kRows * nt), left = mt - g * kRows, h = left < kRows ? left : kRows;
+  const uint32_t in = id - g * kRows * nt;
+  mi = uniform_i32(g * kRows + in % h);
+  ni = uniform_i32(in / h);
 }
 
-// A 256-thread block computes a BM x BN tile, each wave a quarter of it, with
-// two stages of 128 elements of the reduction in LDS.  Rows past an operand's
-// end repeat its last row (their results are not stored); the units past the
+// 16 or 4 bytes a lane from memory to LDS, at lds + lane * 16 or 4 (`lds` the
+// same in every lane).
+__device__ __forceinline__ void load_lds16(rsrc_t r, uint8_t* lds, uint32_t voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16,
+                                           voff, soff, 0, 0);
+}
+__device__ __forceinline__ void load_lds4(rsrc_t r, uint8_t* lds, uint32_t voff, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 4, voff,
+                                           soff, 0, 0);
+}
+
+template <int I>
+struct Part {
+  static constexpr int value = I;
+};
+// f(Part<0>), ..., f(Part<N - 1>).
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void for_parts(const F& f) {
+  if constexpr (I < N) {
+    f(Part<I>{});
+    for_parts<N, I + 1>(f);
+  }
+}
+
+// Waits until at most N of the wave's loads from memory are in flight, or until
+// its LDS reads are done, then for the block's other waves.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_reads() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// A 256-thread block computes a BM x BN tile, each wave a quarter of it, from S
+// slots of 128 elements of the reduction in LDS.  Each half of a step multiplies
+// 64 elements from registers while the next 64 are read from LDS.  Memory is
+// loaded straight to LDS, in whole 128-byte lines, spread evenly over the
+// products: a wave issues in order, and a load that waits for room in the
+// memory pipeline holds up the products behind it.  Rows past an operand's end
+// repeat its last row (their results are not stored); the units past the
 // reduction's end repeat the row's last one and are cleared in LDS.
-template <int BM, int BN, bool PRECISE>
+template <int BM, int BN, int S, bool PRECISE, bool PART>
 __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
-  constexpr int kStage = (BM + BN) * kBK;
-  constexpr int UA = BM / 32, UB = BN / 32;  // loads of 8 rows a wave issues per stage
-  __shared__ __align__(1024) uint8_t lds[2 * kStage];
+  constexpr int kRows = BM + BN;
+  constexpr int kSlot = kRows * kBK;
+  constexpr int kParts = TM + TN;  // fragments of half a step; 64 rows of the tile each
+  constexpr int kCodeUnits = (kRows + 255) / 256;  // of 64 rows' codes, per four steps
+  constexpr int kLoads = 2 * kParts + 1;  // of a wave per step: 8 rows each, and a part of the codes
+  constexpr int kCodes = S * kSlot;       // a word (four steps) a row, two groups of steps
+  // A step's 2 kParts groups of products.  Groups kOpen .. issue its loads.
+  constexpr int kOpen = TM / 2, kOpenB = kParts / 2, kIssue = 2 * kParts - kOpen;
+  static_assert(TM % 2 == 0 && TN % 2 == 0, "two fragments are read at a time");
+  __shared__ __align__(1024) uint8_t lds[kCodes + 2 * kRows * 4];
   const int t = threadIdx.x, lane = t & 63, wave = uniform_i32(t >> 6);
   const int wm = (wave & 1) * WM, wn = (wave >> 1) * WN;
-  const uint32_t nt = static_cast<uint32_t>((p.n + BN - 1) / BN);
-  const uint32_t mi = uniform_i32(blockIdx.x / nt);
-  const int64_t m0 = static_cast<int64_t>(mi) * BM;
-  const int64_t n0 = static_cast<int64_t>(blockIdx.x - mi * nt) * BN;
-  const int steps = static_cast<int>((p.k + kBK - 1) / kBK);
-  const int tail = static_cast<int>(p.k % kBK);
+  uint32_t mi, ni;
+  tile_of(blockIdx.x, static_cast<uint32_t>((p.m + BM - 1) / BM),
+          static_cast<uint32_t>((p.n + BN - 1) / BN), mi, ni);
+  const int64_t m0 = static_cast<int64_t>(mi) * BM, n0 = static_cast<int64_t>(ni) * BN;
+  // this share's steps [first, steps), the first a multiple of four
+  const int all = static_cast<int>((p.k + kBK - 1) / kBK);
+  const int first = PART ? static_cast<int>(blockIdx.y) * p.share : 0;
+  const int steps = PART ? min(all, first + p.share) : all;
+  // elements of a last step that is not whole, or 0
+  const int tail = steps == all ? static_cast<int>(p.k % kBK) : 0;
 
   const rsrc_t ra = make_rsrc(p.a.data + m0 * p.a.ld, -1), rb = make_rsrc(p.b.data + n0 * p.b.ld, -1);
-  uint32_t row_a[UA], row_b[UB];
+  const rsrc_t rca = make_rsrc(p.a.scale + (m0 >> p.a.shift) * p.a.ld_scale, -1);
+  const rsrc_t rcb = make_rsrc(p.b.scale + (n0 >> p.b.shift) * p.b.ld_scale, -1);
+  const int last_a = static_cast<int>(min<int64_t>(BM, p.m - m0)) - 1;
+  const int last_b = static_cast<int>(min<int64_t>(BN, p.n - n0)) - 1;
+  // Load i < 2 kParts covers 8 rows of every wave: together 32 of part i / 2's 64.
+  uint32_t row[2 * kParts], code_row[kCodeUnits];
 #pragma unroll
-  for (int i = 0; i < UA; ++i)
-    row_a[i] = static_cast<uint32_t>(min<int64_t>(8 * (wave + 4 * i) + (lane >> 3), p.m - 1 - m0)) *
-               static_cast<uint32_t>(p.a.ld);
+  for (int i = 0; i < 2 * kParts; ++i) {
+    const int r = 8 * (wave + 4 * i) + (lane >> 3);
+    row[i] = 32 * i < BM ? static_cast<uint32_t>(min(r, last_a)) * static_cast<uint32_t>(p.a.ld)
+                         : static_cast<uint32_t>(min(r - BM, last_b)) * static_cast<uint32_t>(p.b.ld);
+  }
+  const auto code_unit = [&](int i) { return min(wave + 4 * i, kRows / 64 - 1); };
 #pragma unroll
-  for (int i = 0; i < UB; ++i)
-    row_b[i] = static_cast<uint32_t>(min<int64_t>(8 * (wave + 4 * i) + (lane >> 3), p.n - 1 - n0)) *
-               static_cast<uint32_t>(p.b.ld);
+  for (int i = 0; i < kCodeUnits; ++i) {
+    const int r = 64 * code_unit(i) + lane;
+    code_row[i] = 64 * code_unit(i) < BM
+        ? static_cast<uint32_t>(min(r, last_a) >> p.a.shift) * static_cast<uint32_t>(p.a.ld_scale)
+        : static_cast<uint32_t>(min(r - BM, last_b) >> p.b.shift) * static_cast<uint32_t>(p.b.ld_scale);
+  }
 
-  // One stage from memory to LDS, 16 bytes a lane: the lane's place in LDS is
-  // fixed, so it loads the unit that tile_off puts there.
-  const auto load_stage = [&](int kt) {
-    const int soff = kt * kBK;
-    const uint32_t last = kt + 1 == steps && tail ? ((tail + 15) / 16 - 1) * 16u : 112u;
-    uint8_t* const s = lds + (kt & 1) * kStage;
-#pragma unroll
-    for (int i = 0; i < UA + UB; ++i) {
-      const bool a = i < UA;
-      const int unit = wave + 4 * (a ? i : i - UA);
-      const uint32_t c = ((lane & 7) ^ ((4 * unit + (lane >> 4)) & 7)) << 4;
-      const uint32_t voff = (a ? row_a[a ? i : 0] : row_b[a ? 0 : i - UA]) + min(c, last);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          a ? ra : rb,
-          (__attribute__((address_space(3))) void*)(s + (a ? 0 : BM * kBK) + unit * 1024), 16, voff,
-          soff, 0, 0);
-    }
+  // Step kt from memory to a slot, 16 bytes a lane: the lane's place in LDS is
+  // fixed, so it loads the unit that tile_off puts there (past the reduction's
+  // end the last unit that holds anything).
+  const uint32_t unit = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) << 4;
+  const uint32_t last_unit = tail ? ((tail + 15) / 16 - 1) * 16 : 112;
+  const auto load_rows = [&](int kt, int slot, int i) {
+    load_lds16(32 * i < BM ? ra : rb, lds + slot * kSlot + wave * 1024 + i * 4096,
+               row[i] + min(unit, kt + 1 == steps ? last_unit : 112u), kt * kBK);
   };
-  // The stage's bytes past the reduction's end cleared (its last step only).
-  const auto clear_stage = [&](int kt) {
-    uint8_t* const s = lds + (kt & 1) * kStage;
-    for (int r = t; r < BM + BN; r += 256) {
-      const int rr = r < BM ? r : r - BM;
-      uint8_t* const base = s + (r < BM ? 0 : BM * kBK);
-      for (int c = tail / 16; c < 8; ++c) {
-        u32x4* const u = reinterpret_cast<u32x4*>(base + tile_off(rr, c));
-        u32x4 v = *u;
+  const auto load_step = [&](int kt, int slot) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int n = tail - 16 * c - 4 * w;  // bytes of this word that count
-          v[w] = n >= 4 ? v[w] : n <= 0 ? 0u : v[w] & ((1u << (8 * n)) - 1u);
-        }
-        *u = v;
+    for (int i = 0; i < 2 * kParts; ++i) load_rows(kt, slot, i);
+  };
+  // The last step's bytes past the reduction's end cleared, once it has landed.
+  const auto clear_slot = [&](int slot) {
+    __syncthreads();
+    for (int r = t; r < kRows; r += 256)
+      for (int c = tail / 16; c < 8; ++c) {
+        u32x4* const u = reinterpret_cast<u32x4*>(
+            lds + slot * kSlot + (r < BM ? tile_off(r, c) : BM * kBK + tile_off(r - BM, c)));
+        *u = clear_tail(*u, tail - 16 * c);
       }
-    }
     __syncthreads();
   };
-
-  // Codes of four steps at a time, one word a row.
-  const uint8_t* sa_row[TM];
-  const uint8_t* sb_row[TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t r = min<int64_t>(m0 + wm + 32 * i + (lane & 31), p.m - 1);
-    sa_row[i] = p.a.scale + (r >> p.a.shift) * p.a.ld_scale;
-  }
-#pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int64_t r = min<int64_t>(n0 + wn + 32 * j + (lane & 31), p.n - 1);
-    sb_row[j] = p.b.scale + (r >> p.b.shift) * p.b.ld_scale;
-  }
-  uint32_t wa[TM], wb[TN];
-  const auto load_codes = [&](int kt) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) wa[i] = *reinterpret_cast<const uint32_t*>(sa_row[i] + (kt & ~3));
-#pragma unroll
-    for (int j = 0; j < TN; ++j) wb[j] = *reinterpret_cast<const uint32_t*>(sb_row[j] + (kt & ~3));
+  // The codes of the four steps of group g, 64 rows of them.
+  const auto load_codes = [&](int g, int i) {
+    load_lds4(64 * code_unit(i) < BM ? rca : rcb,
+              lds + kCodes + (g & 1) * kRows * 4 + code_unit(i) * 256, code_row[i], 4 * g);
   };
 
   v16f acc[TM][TN];
@@ -171,84 +232,343 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
-  if (steps > 0) {
-    load_codes(0);
-    load_stage(0);
-  }
-  for (int kt = 0; kt < steps; ++kt) {
-    __syncthreads();
-    if (kt + 1 == steps && tail) clear_stage(kt);
-    if (kt > 0 && (kt & 3) == 0) load_codes(kt);
-    if (kt + 1 < steps) load_stage(kt + 1);
-    const int sh = 8 * (kt & 3);
-    const uint8_t* const s = lds + (kt & 1) * kStage;
+  v8i xa[2][TM], yb[2][TN];
+  int ca[TM], cb[TN];
+  Converted<TM, TN> cvt;
+  const auto read_part = [&](int slot, int h, int i) {
+    const uint8_t* const s = lds + slot * kSlot;
+    const int c = 4 * h + 2 * (lane >> 5);
+    const int r = (i < TM ? wm + 32 * i : wn + 32 * (i - TM)) + (lane & 31);
+    const uint8_t* const q = s + (i < TM ? 0 : BM * kBK);
+    const v8i v = join(*reinterpret_cast<const u32x4*>(q + tile_off(r, c)),
+                       *reinterpret_cast<const u32x4*>(q + tile_off(r, c + 1)));
+    if (i < TM) xa[h][i < TM ? i : 0] = v;
+    else yb[h][i < TM ? 0 : i - TM] = v;
+  };
+  const auto read_codes = [&](int kt, int(&ca)[TM], int(&cb)[TN]) {
+    const uint32_t* const w =
+        reinterpret_cast<const uint32_t*>(lds + kCodes + ((kt >> 2) & 1) * kRows * 4) + (lane & 31);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int c = 4 * h + 2 * (lane >> 5);
-      Operand<PRECISE> fa[TM], fb[TN];
+    for (int i = 0; i < TM; ++i) ca[i] = static_cast<int>(w[wm + 32 * i] >> (8 * (kt & 3)));
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const int r = wm + 32 * i + (lane & 31);
-        fa[i].set(*reinterpret_cast<const u32x4*>(s + tile_off(r, c)),
-                  *reinterpret_cast<const u32x4*>(s + tile_off(r, c + 1)), wa[i] >> sh);
-      }
+    for (int j = 0; j < TN; ++j) cb[j] = static_cast<int>(w[BM + wn + 32 * j] >> (8 * (kt & 3)));
+  };
+
+  // Step kt, in 2 kParts groups of products, of its first half and then of its
+  // second.  During the first half's groups its second half is read, two
+  // fragments a group, x's first: when every wave has them, the slot's rows of
+  // x, then those of y, take step kt + S.  During the second half's groups step
+  // kt + 1's first half is read, a fragment a group: its rows of x have landed
+  // at the half's start (behind them, y's and what later steps have issued may still
+  // be in flight), those of y where it reaches them.  Past the last step the
+  // last one is loaded and read again, into a slot that nothing uses: the loop
+  // has no branch.  The codes of the next four steps are loaded one part a step.
+  const int last_group = (steps - 1) >> 2;
+  if (first < steps) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int r = wn + 32 * j + (lane & 31);
-        fb[j].set(*reinterpret_cast<const u32x4*>(s + BM * kBK + tile_off(r, c)),
-                  *reinterpret_cast<const u32x4*>(s + BM * kBK + tile_off(r, c + 1)), wb[j] >> sh);
-      }
+    for (int i = 0; i < kCodeUnits; ++i) load_codes(first >> 2, i);
+    load_step(first, 0);
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[i][j] = mma(fb[j], wb[j] >> sh, fa[i], wa[i] >> sh, acc[i][j]);
+    for (int i = 1; i < S; ++i) {
+      load_step(min(first + i, steps - 1), i);
+      load_codes(min((first >> 2) + 1, last_group), 0);
     }
+    wait_loads<(S - 1) * kLoads>();
+    if (tail && first + 1 == steps) clear_slot(0);
+    read_codes(first, ca, cb);
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) read_part(0, 0, i);
   }
+  int slot = 0;
+  for (int kt = first; kt < steps; ++kt) {
+    const int next = slot + 1 == S ? 0 : slot + 1, ahead = min(kt + S, steps - 1);
+    // loads [g kLoads / kIssue, (g + 1) kLoads / kIssue) of step kt + S
+    const auto issue = [&](auto g) {
+      if constexpr (g.value >= 0)
+#pragma unroll
+        for (int i = g.value * kLoads / kIssue; i < (g.value + 1) * kLoads / kIssue; ++i) {
+          if (i < 2 * kParts) load_rows(ahead, slot, i);
+          else load_codes(min((kt >> 2) + 1, last_group), kCodeUnits == 1 ? 0 : kt & 1);
+        }
+    };
+    for_parts<kParts>([&](auto g) {
+      if constexpr (2 * g.value < kParts) {
+        read_part(slot, 1, 2 * g.value);
+        read_part(slot, 1, 2 * g.value + 1);
+      }
+      if constexpr (g.value == kOpen || g.value == kOpenB) wait_reads();
+      issue(Part<g.value - kOpen>{});
+      mma<PRECISE, g.value>(xa[0], ca, yb[0], cb, acc, cvt);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    int na[TM], nb[TN];
+    for_parts<kParts>([&](auto g) {
+      // loads of steps past kt + 1 issued before this group
+      constexpr int issued = (S - 2) * kLoads + (kParts + g.value - kOpen) * kLoads / kIssue;
+      if constexpr (g.value == 0) {
+        wait_loads<kLoads - 2 * TM + issued>();
+        if (tail && kt + 2 == steps) clear_slot(next);
+        read_codes(kt + 1, na, nb);
+      }
+      if constexpr (g.value == TM) wait_loads<issued>();
+      read_part(next, 0, g.value);
+      issue(Part<kParts + g.value - kOpen>{});
+      mma<PRECISE, g.value>(xa[1], ca, yb[1], cb, acc, cvt);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+#pragma unroll
+    for (int i = 0; i < TM; ++i) ca[i] = na[i];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) cb[j] = nb[j];
+    slot = next;
+  }
+  __syncthreads();
 
   // A lane holds 4 consecutive columns of a row at a time; through LDS, 32
   // rows of the wave's tile at a time, the rows become contiguous.
-  __syncthreads();
-  constexpr int kPitch = WN + 4;  // floats
-  static_assert(4 * 32 * kPitch * 4 <= 2 * kStage, "the waves' slabs fit the stages");
-  float* const slab = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
+  typedef typename std::conditional<PRECISE || PART, float, uint16_t>::type Out;
+  constexpr int kPer = 16 / sizeof(Out);             // elements of a 16-byte store
+  constexpr int kPitch = WN + kPer;
+  static_assert(4 * 32 * kPitch * sizeof(Out) <= S * kSlot, "the waves' slabs fit the slots");
+  Out* const slab = reinterpret_cast<Out*>(lds) + wave * 32 * kPitch;
+  Out* const out = static_cast<Out*>(p.out) + (PART ? blockIdx.y * p.m * p.ld_out : 0) +
+                   (m0 + wm) * p.ld_out + n0 + wn;
+  const int64_t rows = p.m - m0 - wm, cols = p.n - n0 - wn;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
-        const int col = 32 * j + 2 * e + 4 * (lane >> 5);
-        *reinterpret_cast<float4*>(slab + (lane & 31) * kPitch + col) =
-            float4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        Out* const q = slab + (lane & 31) * kPitch + 32 * j + 2 * e + 4 * (lane >> 5);
+        if constexpr (sizeof(Out) == 4) {
+          *reinterpret_cast<v4f*>(q) = v4f{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        } else {
+          const v4b v = __builtin_convertvector(
+              (v4f{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]}), v4b);
+          *reinterpret_cast<v4b*>(q) = v;
+        }
       }
     __builtin_amdgcn_wave_barrier();
+    constexpr int kRun = WN / kPer, kStep = 64 / kRun;  // lanes of a row, rows of a store
+    const int c = lane % kRun * kPer;
+    if (rows >= 32 * (i + 1) && cols >= WN) {
 #pragma unroll
-    for (int u = lane; u < 32 * (WN / 8); u += 64) {
-      const int r = u / (WN / 8), c = u % (WN / 8) * 8;
-      float v[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = slab[r * kPitch + c + q];
-      const int64_t row = m0 + wm + 32 * i + r, col = n0 + wn + c;
-      if (row < p.m) put8(p.out, row * p.ld_out + col, p.n - col, p.out_f32, v);
+      for (int r = 0; r < 32; r += kStep) {
+        const int rr = r + lane / kRun;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(slab + rr * kPitch + c);
+        *reinterpret_cast<u32x4_h*>(out + (32 * i + rr) * p.ld_out + c) = v;
+      }
+    } else {
+#pragma unroll 1
+      for (int r = lane / kRun; r < 32 && 32 * i + r < rows; r += kStep)
+#pragma unroll 1
+        for (int q = 0; q < kPer && c + q < cols; ++q)
+          out[(32 * i + r) * p.ld_out + c + q] = slab[r * kPitch + c + q];
     }
     __builtin_amdgcn_wave_barrier();
   }
 }
 
+// out = the sum of `shares` partial results, in order (row by row of n, which
+// the partial results are stored in without padding).
+template <typename Out>
+__global__ __launch_bounds__(256) void matmul_join_kernel(const float* __restrict__ part,
+                                                          int32_t shares, int64_t m, int64_t n,
+                                                          Out* __restrict__ out, int64_t ld_out) {
+  const int64_t size = m * n;
+  for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8; i < size;
+       i += static_cast<int64_t>(gridDim.x) * 256 * 8) {
+    float v[8], w[8];
+    load8(part + i, size - i, v);
+    for (int32_t q = 1; q < shares; ++q) {
+      load8(part + q * size + i, size - i, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += w[j];
+    }
+    const int64_t row = i / n, col = i - row * n;
+    if (col + 8 <= n) {
+      store8(out + row * ld_out + col, 8, v);
+    } else {  // the run ends in a later row
+      int64_t r = row, c = col;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (i + j < size) store8(out + r * ld_out + c, 1, {v[j], 0, 0, 0, 0, 0, 0, 0});
+        if (++c == n) {
+          c = 0;
+          ++r;
+        }
+      }
+    }
+  }
+}
+
+// Up to 16 rows of a (tokens): every element of b is read once, straight to
+// registers, and little else counts.  A block takes 16 rows of b; its waves take
+// shares of the reduction, each with the loads of U steps in flight, and their
+// sums are added in order.  a's rows past its end repeat the last one.  16 x 16
+// products: b's rows along the accumulator's registers, a's along its lanes.
+template <int W, int U, bool PRECISE>
+__global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p) {
+  __shared__ float sums[W][4][64];
+  const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 16;
+  const int steps = static_cast<int>((p.k + kBK - 1) / kBK), tail = static_cast<int>(p.k % kBK);
+  const int per = (steps + W - 1) / W;
+  const int k0 = wave * per, k1 = min(steps, k0 + per);
+
+  const rsrc_t rb = make_rsrc(p.b.data + n0 * p.b.ld, -1), ra = make_rsrc(p.a.data, -1);
+  const int64_t qa = min<int64_t>(r, p.m - 1), qb = min<int64_t>(n0 + r, p.n - 1);
+  const uint32_t row_a = static_cast<uint32_t>(qa) * static_cast<uint32_t>(p.a.ld);
+  const uint32_t row_b = static_cast<uint32_t>(qb - n0) * static_cast<uint32_t>(p.b.ld);
+  const uint8_t* const code_a = p.a.scale + (qa >> p.a.shift) * p.a.ld_scale;
+  const uint8_t* const code_b = p.b.scale + (qb >> p.b.shift) * p.b.ld_scale;
+  v4f acc = {0, 0, 0, 0};
+  for (int kt = k0; kt < k1; kt += U) {
+    u32x4 a[U][2], b[U][2];
+    int ca[U], cb[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {  // (steps past the share's end repeat its last one, unused)
+      const int ks = min(kt + u, k1 - 1);
+      const uint32_t last = tail && ks + 1 == steps ? ((tail + 15) / 16 - 1) * 16u : 112u;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t c = min<uint32_t>(32 * g + 16 * h, last);
+        b[u][h] = buf_b128(rb, row_b + c, ks * kBK);
+        a[u][h] = buf_b128(ra, row_a + c, ks * kBK);
+      }
+      cb[u] = code_b[ks];
+      ca[u] = code_a[ks];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (kt + u >= k1) break;
+      if (tail && kt + u + 1 == steps) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          b[u][h] = clear_tail(b[u][h], tail - 32 * g - 16 * h);
+          a[u][h] = clear_tail(a[u][h], tail - 32 * g - 16 * h);
+        }
+      }
+      const v8i x = join(a[u][0], a[u][1]), y = join(b[u][0], b[u][1]);
+      if constexpr (!PRECISE) {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(y, x, acc, 0, 0, 0, cb[u], 0, ca[u]);
+      } else {
+        v8b xb[4], yb[4];
+        to_bf16(x, ca[u], xb);
+        to_bf16(y, cb[u], yb);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yb[q], xb[q], acc, 0, 0, 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sums[wave][e][lane] = acc[e];
+  __syncthreads();
+  // result (row, col): row = lane % 16, col = 4 (lane / 16) + e
+  for (int q = threadIdx.x; q < 256; q += 64 * W) {
+    const int col = q & 15, row = q >> 4, e = col & 3, l = row + 16 * (col >> 2);
+    float v = sums[0][e][l];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v += sums[w][e][l];
+    if (row < p.m && n0 + col < p.n) {
+      const int64_t at = row * p.ld_out + n0 + col;
+      if constexpr (PRECISE) static_cast<float*>(p.out)[at] = v;
+      else static_cast<uint16_t*>(p.out)[at] = round_bf16(v);
+    }
+  }
+}
+
+// ---- choice of a form --------------------------------------------------------
+
+constexpr int64_t kRowsMax = 16;  // rows of a up to which matmul_rows_kernel is taken
+
+int64_t tiles(const int64_t m, const int64_t n, int bm, int bn) {
+  return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
+}
+
+// Shares of the reduction for 128 x 128 tiles that do not fill the 256 CUs.
+int shares(int64_t m, int64_t n, int64_t k) {
+  if (m <= kRowsMax) return 1;
+  const int64_t t = tiles(m, n, 128, 128), steps = (k + kBK - 1) / kBK;
+  if (t > 160) return 1;
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= 16 && s * t <= 512; ++s) {
+    const int64_t per = ((steps + s - 1) / s + 3) / 4 * 4;  // (codes come four steps at a time)
+    if ((s - 1) * per >= steps && s > 1) continue;
+    const double us = static_cast<double>(per) * (s * t > 256 ? 0.58 : 0.42) +
+                      (s > 1 ? 3.0 + 8.0 * s * m * n / 6e6 : 0.0);
+    if (us < least) {
+      least = us;
+      best = s;
+    }
+  }
+  return best;
+}
+
+template <bool PRECISE>
+void launch_rows(const MatmulArgs& a, hipStream_t s) {
+#define ZF_ROWS(W, U)                                                                   \
+  hipLaunchKernelGGL((matmul_rows_kernel<W, U, PRECISE>), dim3(static_cast<uint32_t>(blocks)), \
+                     dim3(64 * W), 0, s, a)
+  const int64_t blocks = (a.n + 15) / 16;
+  if (blocks >= 512) ZF_ROWS(4, 8);
+  else if (blocks >= 128) ZF_ROWS(8, 4);
+  else ZF_ROWS(16, 4);
+#undef ZF_ROWS
+}
+
+template <bool PRECISE>
+void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
+#define ZF_TILES(BM, BN, S, PART, Y, ARGS)                                                       \
+  hipLaunchKernelGGL((matmul_tile_kernel<BM, BN, S, PRECISE, PART>),                             \
+                     dim3(static_cast<uint32_t>(tiles(a.m, a.n, BM, BN)), Y), dim3(256), 0, s, ARGS)
+  if (!PRECISE && tiles(a.m, a.n, 256, 256) >= 160) {
+    if constexpr (!PRECISE) ZF_TILES(256, 256, 2, false, 1, a);
+  } else if (tiles(a.m, a.n, 128, 256) >= 160) {
+    ZF_TILES(128, 256, 2, false, 1, a);
+  } else if (const int q = shares(a.m, a.n, a.k); q > 1) {
+    MatmulArgs b = a;
+    b.out = ws;
+    b.ld_out = a.n;
+    const int64_t steps = (a.k + kBK - 1) / kBK;
+    b.share = static_cast<int32_t>(((steps + q - 1) / q + 3) / 4 * 4);
+    ZF_TILES(128, 128, 2, true, q, b);
+    const int64_t blocks = (a.m * a.n + 2047) / 2048;
+    const dim3 grid(static_cast<uint32_t>(blocks < 2048 ? blocks : 2048));
+    if (PRECISE)
+      hipLaunchKernelGGL((matmul_join_kernel<float>), grid, dim3(256), 0, s,
+                         static_cast<const float*>(ws), q, a.m, a.n, static_cast<float*>(a.out),
+                         a.ld_out);
+    else
+      hipLaunchKernelGGL((matmul_join_kernel<uint16_t>), grid, dim3(256), 0, s,
+                         static_cast<const float*>(ws), q, a.m, a.n, static_cast<uint16_t*>(a.out),
+                         a.ld_out);
+  } else {
+    ZF_TILES(128, 128, 2, false, 1, a);
+  }
+#undef ZF_TILES
+}
+
 }  // namespace
 
-size_t matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
+size_t matmul_workspace(int64_t m, int64_t n, int64_t k) {
+  const int q = shares(m, n, k);
+  return q > 1 ? static_cast<size_t>(q) * m * n * sizeof(float) : 0;
+}
 
-hipError_t launch_matmul(const MatmulArgs& a, void*, hipStream_t s) {
+hipError_t launch_matmul(const MatmulArgs& a, void* ws, hipStream_t s) {
   (void)hipGetLastError();
-  const auto tiles = [&](int bm, int bn) {
-    return dim3(static_cast<uint32_t>(((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn)));
-  };
-  if (a.out_f32)
-    hipLaunchKernelGGL((matmul_tile_kernel<128, 128, true>), tiles(128, 128), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((matmul_tile_kernel<128, 128, false>), tiles(128, 128), dim3(256), 0, s, a);
+  if (a.m <= kRowsMax) {
+    if (a.out_f32) launch_rows<true>(a, s);
+    else launch_rows<false>(a, s);
+  } else {
+    if (a.out_f32) launch_tiles<true>(a, ws, s);
+    else launch_tiles<false>(a, ws, s);
+  }
   return hipGetLastError();
 }
 

@@ -107,7 +107,7 @@ def largest(a, b):
     """The sum over every 64 elements of the reduction of the largest product's
     magnitude."""
     a, b = a.abs(), b.abs()
-    out = torch.zeros(a.shape[0], b.shape[0], dtype=torch.float64)
+    out = torch.zeros(a.shape[0], b.shape[0], dtype=torch.float64, device=a.device)
     for k in range(0, a.shape[1], 64):
         x, y = a[:, k:k + 64], b[:, k:k + 64]
         for r in range(0, a.shape[0], 32):
@@ -117,6 +117,7 @@ def largest(a, b):
 
 def product_check(a, b, a64, b64, dtype, out=None):
     k = a64.shape[1]
+    a64, b64 = a64.cuda(), b64.cuda()
     got = zf.matmul_fp8(a, b, out=out, dtype=dtype)
     torch.cuda.synchronize()
     want = a64 @ b64.t()
@@ -124,7 +125,7 @@ def product_check(a, b, a64, b64, dtype, out=None):
     tol = (k / 16 + 8) * 2.0 ** -23 * size
     if dtype == torch.bfloat16:
         tol = tol + 2.0 ** -8 * want.abs() + 2.0 ** -10 * largest(a64, b64)
-    err = (got.double().cpu() - want).abs()
+    err = (got.double() - want).abs()
     assert (err <= tol).all(), (err - tol).max()
     return got
 
@@ -141,6 +142,24 @@ def test_matmul(m, n, k, groups, dtype):
     assert (buf[m:] == 7.0).all() and (buf[:, n:] == 7.0).all(), "written outside"
     again = zf.matmul_fp8(a, b, dtype=dtype)
     assert torch.equal(again, got), "equal calls give equal bits"
+
+
+# Enough tiles for the larger tile shapes (256 x 256 and, below, 128 x 256), with
+# reductions of one step, of odd ends, of whole steps.
+LARGE = [(4100, 2700, k) for k in (1, 65, 128, 129, 500, 640)] + \
+        [(2100, 2600, k) for k in (16, 127, 256, 1100)] + [(5000, 2100, 384), (1300, 4000, 777)]
+
+
+@pytest.mark.parametrize("m,n,k", LARGE)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_matmul_large(m, n, k, dtype):
+    gen = torch.Generator().manual_seed(m + n + k)
+    a, a64 = R.random_fp8(zf, m, k, 1, gen)
+    b, b64 = R.random_fp8(zf, n, k, 128 if k % 2 else 1, gen)
+    buf = torch.full((m + 1, n + 5), 7.0, dtype=dtype, device="cuda")
+    got = product_check(a, b, a64, b64, dtype, out=buf[:m, :n])
+    assert (buf[m:] == 7.0).all() and (buf[:, n:] == 7.0).all(), "written outside"
+    assert torch.equal(zf.matmul_fp8(a, b, dtype=dtype), got), "equal calls give equal bits"
 
 
 def test_matmul_empty():
