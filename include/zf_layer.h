@@ -64,8 +64,8 @@ typedef struct zf_fp8 {
 /* x [rows][ld_x] (bf16 or fp32) to 8 bits: `out` receives x, `out_t` its
  * transpose (an operand of cols rows and rows columns, whose groups run along
  * x's rows).  Either may be NULL, not both; they share one `group`.  With
- * group 128 both hold the same values.  rows, cols < 2^30.  Bytes of the
- * outputs past their columns are not written. */
+ * group 128 both hold the same values.  rows, cols < 2^30, fewer than 2^24
+ * tiles of 128 x 128.  Bytes of the outputs past their columns are not written. */
 zf_status zf_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t cols,
                           int64_t ld_x, const zf_fp8* out, const zf_fp8* out_t,
                           zf_stream stream);
@@ -89,7 +89,7 @@ size_t zf_matmul_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k);
  * with an fp32 result products and sums are fp32, values of a or b (elements
  * times scales) below 2^-126 may count as zero and those past bf16's range as
  * infinities.  m, n < 2^30; k and, with more than
- * one row, both ld_data < 2^23; at most 2^24 tiles of 128 x 128.  ws: zf_matmul_fp8_workspace_bytes(m, n, k) bytes,
+ * one row, both ld_data < 2^23; fewer than 2^24 tiles of 128 x 128.  ws: zf_matmul_fp8_workspace_bytes(m, n, k) bytes,
  * 16-byte aligned (may be NULL if that is 0), contents overwritten. */
 zf_status zf_matmul_fp8(const zf_fp8* a, const zf_fp8* b, int64_t m, int64_t n, int64_t k,
                         void* out, int32_t out_dtype, int64_t ld_out, void* ws, size_t ws_bytes,
@@ -163,7 +163,7 @@ typedef struct zf_adamw_plan zf_adamw_plan;
 /* Device bytes of a plan over these tensors (its tables).  tensors: HOST
  * array of count >= 1; 32- and 8-bit states and both gradient types may be
  * mixed.  Every pointer is aligned to its element; no two buffers overlap.
- * Together fewer than 2^35 elements (one launch). */
+ * Together fewer than 2^34 elements (one launch). */
 zf_status zf_adamw_plan_query(const zf_adamw_tensor* tensors, int32_t count,
                               size_t* device_bytes);
 

@@ -1,7 +1,10 @@
 // AdamW over many tensors in one launch (formulas in zf_layer.h).
 //
-// A 256-thread block takes kAdamwChunk consecutive elements of one tensor; the
-// plan's table of block offsets says which.  32 lanes hold one 128-element
+// A 256-thread block takes a chunk of consecutive elements of one tensor, 2048 of
+// one with 8-bit states, 1024 of one with 32-bit states; the plan's table of block
+// offsets says which.  (202 M elements in us, chunks of 1024 / 2048 / 4096: 8-bit
+// 618 / 587 / 637, 32-bit 941 / 990 / 1013.  Remapping blocks to XCDs changes
+// nothing: no line is shared.)  32 lanes hold one 128-element
 // block of the 8-bit states, 4 elements a lane, so that every stream is read
 // and written in contiguous lines: its largest magnitudes are taken over those
 // lanes and the codes written in the same pass.  Bound by HBM: 28 bytes per
@@ -11,8 +14,6 @@
 
 namespace zf {
 namespace {
-
-constexpr int kQuads = kAdamwChunk / (256 * 4);  // of 4 elements a thread
 
 __device__ __forceinline__ u32x4 load4_f32(const float* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const u32x4_f*>(p));
@@ -125,6 +126,7 @@ __device__ __forceinline__ uint32_t encode4(const float (&x)[4], float* scale) {
 template <typename G>
 __device__ __forceinline__ void adamw_f32(const AdamTensor& t, int64_t base, const AdamK& c,
                                           float gs, bool scaled) {
+  constexpr int kQuads = kAdamwChunk32 / (256 * 4);
   float g[kQuads][4], p[kQuads][4], m[kQuads][4], v[kQuads][4];
   float* const mp = static_cast<float*>(t.m);
   float* const vp = static_cast<float*>(t.v);
@@ -152,6 +154,7 @@ __device__ __forceinline__ void adamw_f32(const AdamTensor& t, int64_t base, con
 template <typename G>
 __device__ __forceinline__ void adamw_8bit(const AdamTensor& t, int64_t base, const AdamK& c,
                                            float gs, bool scaled) {
+  constexpr int kQuads = kAdamwChunk8 / (256 * 4);
   float g[kQuads][4], p[kQuads][4], ms[kQuads], vs[kQuads];
   uint32_t mq[kQuads], vq[kQuads];
   uint8_t* const mp = static_cast<uint8_t*>(t.m);
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamTensor* __restrict
     t.vs = s->vs;
     t.grad_f32 = s->grad_f32;
   }
-  const int64_t base = (b - o[lo]) * kAdamwChunk;
+  const int64_t base = (b - o[lo]) * (t.ms != nullptr ? kAdamwChunk8 : kAdamwChunk32);
   const bool scaled = grad_scale != nullptr;
   const float gs = scaled ? *grad_scale : 1.0f;
   if (t.ms != nullptr) {

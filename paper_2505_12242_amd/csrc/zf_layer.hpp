@@ -94,7 +94,8 @@ struct AdamTensor {
   int32_t grad_f32;
   int32_t pad;
 };
-constexpr int kAdamwChunk = 4096;  // elements per block
+constexpr int kAdamwChunk8 = 2048;  // elements per block, states in 8 bits
+constexpr int kAdamwChunk32 = 1024;  // and in 32
 hipError_t launch_adamw(const AdamTensor* tensors, const int64_t* off, int32_t count,
                         int64_t blocks, const AdamK& c, const float* grad_scale, hipStream_t s);
 
@@ -104,71 +105,93 @@ hipError_t launch_adamw(const AdamTensor* tensors, const int64_t* off, int32_t c
 // fp32 elements at any 4-byte alignment, 16 bytes a lane (see u32x4_h for bf16).
 typedef u32x4 u32x4_f __attribute__((aligned(4)));
 
-// Elements p[0 .. 8) as fp32; those at and past `valid` are 0 and not read.
-__device__ __forceinline__ void load8(const uint16_t* p, int64_t valid, float (&v)[8]) {
-  if (valid >= 8) {
-    const u32x4 u = *reinterpret_cast<const u32x4_h*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(u[i] << 16);
-      v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? widen_bf16(p[i]) : 0.0f;
-  }
-}
-__device__ __forceinline__ void load8(const float* p, int64_t valid, float (&v)[8]) {
-  if (valid >= 8) {
-    const u32x4 a = *reinterpret_cast<const u32x4_f*>(p);
-    const u32x4 b = *reinterpret_cast<const u32x4_f*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = __uint_as_float(a[i]);
-      v[4 + i] = __uint_as_float(b[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.0f;
-  }
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Two values to bf16, to nearest, ties to even.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
 }
 
-// v rounded to the type of p and stored at p[0 .. min(valid, 8)).
-__device__ __forceinline__ void store8(uint16_t* p, int64_t valid, const float (&v)[8]) {
-  if (valid >= 8) {
-    u32x4 u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      u[i] = round_bf16(v[2 * i]) | (static_cast<uint32_t>(round_bf16(v[2 * i + 1])) << 16);
-    *reinterpret_cast<u32x4_h*>(p) = u;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < valid) p[i] = round_bf16(v[i]);
-  }
-}
-__device__ __forceinline__ void store8(float* p, int64_t valid, const float (&v)[8]) {
-  if (valid >= 8) {
-    u32x4 a, b;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      a[i] = __float_as_uint(v[i]);
-      b[i] = __float_as_uint(v[4 + i]);
-    }
-    *reinterpret_cast<u32x4_f*>(p) = a;
-    *reinterpret_cast<u32x4_f*>(p + 4) = b;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < valid) p[i] = v[i];
-  }
-}
+// Eight elements as they are stored: loaded and stored with as few accesses as
+// any element alignment allows, widened where they are used.  Elements at and
+// past `valid` are zeros, neither read nor written.  NT: read or written once.
+template <typename T>
+struct Vec8;
 
-// A value as its storage type holds it.
-__device__ __forceinline__ float as_stored(const uint16_t*, float v) {
-  return widen_bf16(round_bf16(v));
-}
-__device__ __forceinline__ float as_stored(const float*, float v) { return v; }
+template <>
+struct Vec8<uint16_t> {
+  u32x4 u;
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const uint16_t* p, int64_t valid) {
+    if (valid >= 8) {
+      u = NT ? load8_bf16(p) : *reinterpret_cast<const u32x4_h*>(p);
+    } else {
+      u = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < valid) u[j >> 1] |= static_cast<uint32_t>(p[j]) << (16 * (j & 1));
+    }
+  }
+  template <bool NT = false>
+  __device__ __forceinline__ void store(uint16_t* p, int64_t valid) const {
+    if (valid >= 8) {
+      if (NT) store8_bf16(p, u);
+      else *reinterpret_cast<u32x4_h*>(p) = u;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < valid) p[j] = static_cast<uint16_t>(u[j >> 1] >> (16 * (j & 1)));
+    }
+  }
+  __device__ __forceinline__ float operator[](int j) const {
+    return __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {  // rounded
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+  }
+};
+
+template <>
+struct Vec8<float> {
+  u32x4 u[2];
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const float* p, int64_t valid) {
+    if (valid >= 8) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const u32x4_f* const q = reinterpret_cast<const u32x4_f*>(p + 4 * i);
+        u[i] = NT ? __builtin_nontemporal_load(q) : *q;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[j >> 2][j & 3] = j < valid ? __float_as_uint(p[j]) : 0u;
+    }
+  }
+  template <bool NT = false>
+  __device__ __forceinline__ void store(float* p, int64_t valid) const {
+    if (valid >= 8) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        u32x4_f* const q = reinterpret_cast<u32x4_f*>(p + 4 * i);
+        if (NT) __builtin_nontemporal_store(u[i], q);
+        else *q = u[i];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < valid) p[j] = __uint_as_float(u[j >> 2][j & 3]);
+    }
+  }
+  __device__ __forceinline__ float operator[](int j) const {
+    return __uint_as_float(u[j >> 2][j & 3]);
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j >> 2][j & 3] = __float_as_uint(v[j]);
+  }
+};
 
 // The largest x of the calling lane's 16 (lanes 16i .. 16i + 15), in each of
 // them.  Magnitudes are compared as bit patterns, in which a NaN is largest.
@@ -192,26 +215,57 @@ __device__ __forceinline__ uint32_t fp8_code(uint32_t bits) {
   const uint32_t e = (bits + 0x1fffffu) >> 23;
   return e > 8u ? e - 8u : 0u;
 }
-// What a group's elements are multiplied by: 2^(127 - code), an exact
-// operation but for results below 2^-126, which round to code 0 either way.
-__device__ __forceinline__ float fp8_mult(uint32_t code) {
-  return __uint_as_float((254u - (code < 255u ? code : 254u)) << 23);
-}
-
 // Four values of magnitude <= 448 (plus rounding) to e4m3, ties to even.
 __device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d) {
-  int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  const int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, u, true));
 }
 
-// Eight values of a group to e4m3 codes.
+// The scale of a code, as the conversions below take it (its exponent bits).
+__device__ __forceinline__ float fp8_scale(uint32_t code) { return __uint_as_float(code << 23); }
+
+// Eight values of a group over its scale to e4m3, to nearest, ties to even;
+// zeros where the group holds an infinity or a NaN.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u32x2 quant8(const float (&v)[8], uint32_t code) {
-  const float f = fp8_mult(code);
+  const float s = fp8_scale(code);
   u32x2 u;
-  u.x = pack_fp8(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-  u.y = pack_fp8(v[4] * f, v[5] * f, v[6] * f, v[7] * f);
-  if (code == 255u) u = u32x2{0u, 0u};
-  return u;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    i16x2 q = {0, 0};
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, v[4 * i], v[4 * i + 1], s, false);
+    q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, v[4 * i + 2], v[4 * i + 3], s, true);
+    u[i] = __builtin_bit_cast(uint32_t, q);
+  }
+  return code == 255u ? u32x2{0u, 0u} : u;
+}
+// The same of bf16 values, two a word.
+__device__ __forceinline__ u32x2 quant8_bf16(uint32_t a, uint32_t b, uint32_t c, uint32_t d,
+                                             uint32_t code) {
+  const float s = fp8_scale(code);
+  i16x2 q = {0, 0}, r = {0, 0};
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, a), s, false);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, b), s, true);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, c), s, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, d), s, true);
+  const u32x2 u = {__builtin_bit_cast(uint32_t, q), __builtin_bit_cast(uint32_t, r)};
+  return code == 255u ? u32x2{0u, 0u} : u;
+}
+
+// A group's magnitudes, and its elements in 8 bits.
+template <typename T>
+__device__ __forceinline__ uint32_t abs_max(const Vec8<T>& v) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+  return m;
+}
+__device__ __forceinline__ u32x2 quant8(const Vec8<uint16_t>& v, uint32_t code) {
+  return quant8_bf16(v.u[0], v.u[1], v.u[2], v.u[3], code);
+}
+__device__ __forceinline__ u32x2 quant8(const Vec8<float>& v, uint32_t code) {
+  const float w[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+  return quant8(w, code);
 }
 
 // Bytes p[0 .. min(valid, 8)); p is 8-byte aligned.

@@ -103,7 +103,9 @@ zf_status zf_quantize_fp8(const void* x, int32_t x_dtype, int64_t rows, int64_t 
   Fp8Spans q, qt;
   if (out != nullptr) q = fp8_spans(out, rows, cols, ok);
   if (out_t != nullptr) qt = fp8_spans(out_t, cols, rows, ok);
-  if (!ok || !disjoint({q.data, q.scale, qt.data, qt.scale}, {sx})) return ZF_EINVAL;
+  if (!ok || ceil_div(rows, 128) * ceil_div(cols, 128) >= kGridLimit ||
+      !disjoint({q.data, q.scale, qt.data, qt.scale}, {sx}))
+    return ZF_EINVAL;
   if (rows == 0 || cols == 0) return ZF_OK;
   const zf::QuantArgs a{x, rows, cols, ld_x, fp8_out(out), fp8_out(out_t)};
   return done(zf::launch_quantize(a, x_dtype, (out != nullptr ? out : out_t)->group,
@@ -242,12 +244,16 @@ size_t adamw_bytes(int32_t count) {
   return static_cast<size_t>(count) * (sizeof(zf::AdamTensor) + sizeof(int64_t));
 }
 
+int64_t adamw_chunks(const zf_adamw_tensor& t) {
+  return ceil_div(t.n, t.exp_avg_scale != nullptr ? zf::kAdamwChunk8 : zf::kAdamwChunk32);
+}
+
 bool adamw_tensor_ok(const zf_adamw_tensor& t) {
   if (t.n < 0 || !dtype_ok(t.grad_dtype)) return false;
   const bool eight = t.exp_avg_scale != nullptr;
   if (eight != (t.exp_avg_sq_scale != nullptr) && t.n > 0) return false;
   if (t.n == 0) return true;
-  if (t.n >= kGridLimit * zf::kAdamwChunk) return false;
+  if (t.n >= kGridLimit * zf::kAdamwChunk32) return false;
   const size_t state = eight ? 1 : 4;
   return t.grad != nullptr && aligned(t.grad, dtype_size(t.grad_dtype)) && t.master != nullptr &&
          aligned(t.master, 4) && aligned(t.weight, 2) && t.exp_avg != nullptr &&
@@ -267,7 +273,7 @@ int64_t adamw_blocks(const zf_adamw_tensor* tensors, int32_t count) {
   for (int32_t i = 0; i < count; ++i) {
     const zf_adamw_tensor& t = tensors[i];
     if (!adamw_tensor_ok(t)) return -1;
-    blocks += ceil_div(t.n, zf::kAdamwChunk);
+    blocks += adamw_chunks(t);
     if (blocks >= kGridLimit) return -1;
     if (t.n == 0) continue;
     const bool eight = t.exp_avg_scale != nullptr;
@@ -329,7 +335,7 @@ zf_status zf_adamw_plan_create(const zf_adamw_tensor* tensors, int32_t count, vo
   for (int32_t i = 0; i < count; ++i) {
     const zf_adamw_tensor& t = tensors[i];
     off[i] = at;
-    at += ceil_div(t.n, zf::kAdamwChunk);
+    at += adamw_chunks(t);
     dev[i] = zf::AdamTensor{t.n, t.grad, t.master, t.weight, t.exp_avg, t.exp_avg_sq,
                             t.exp_avg_scale, t.exp_avg_sq_scale, t.grad_dtype == ZF_F32 ? 1 : 0,
                             0};

@@ -379,24 +379,29 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const float* __restric
   const int64_t size = m * n;
   for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8; i < size;
        i += static_cast<int64_t>(gridDim.x) * 256 * 8) {
-    float v[8], w[8];
-    load8(part + i, size - i, v);
-    for (int32_t q = 1; q < shares; ++q) {
-      load8(part + q * size + i, size - i, w);
+    float v[8] = {};
+    for (int32_t q = 0; q < shares; ++q) {
+      Vec8<float> w;
+      w.load(part + q * size + i, size - i);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += w[j];
+      for (int j = 0; j < 8; ++j) v[j] = q == 0 ? w[j] : v[j] + w[j];
     }
-    const int64_t row = i / n, col = i - row * n;
+    int64_t row = i / n, col = i - row * n;
+    Vec8<Out> o;
+    o.set(v);
     if (col + 8 <= n) {
-      store8(out + row * ld_out + col, 8, v);
+      o.store(out + row * ld_out + col, 8);
     } else {  // the run ends in a later row
-      int64_t r = row, c = col;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (i + j < size) store8(out + r * ld_out + c, 1, {v[j], 0, 0, 0, 0, 0, 0, 0});
-        if (++c == n) {
-          c = 0;
-          ++r;
+        if (i + j < size) {
+          const float one[8] = {v[j]};
+          o.set(one);
+          o.store(out + row * ld_out + col, 1);
+        }
+        if (++col == n) {
+          col = 0;
+          ++row;
         }
       }
     }

@@ -12,6 +12,8 @@
 // of rows each and keep their columns' sums in registers; the blocks' partial
 // sums are added in block order by a second kernel, so the result does not
 // depend on timing.
+#include <algorithm>
+
 #include "zf_layer.hpp"
 
 namespace zf {
@@ -37,73 +39,74 @@ __device__ __forceinline__ float block_sum(float x, float (&red)[NT / 64]) {
   return s;
 }
 
-__device__ __forceinline__ void load_gain(const NormArgs& a, int64_t c, int64_t valid,
-                                          float (&g)[8]) {
-  if (a.gain_f32) load8(static_cast<const float*>(a.gain) + c, valid, g);
-  else load8(static_cast<const uint16_t*>(a.gain) + c, valid, g);
-}
-__device__ __forceinline__ void load_gain(const NormBwdArgs& a, int64_t c, int64_t valid,
-                                          float (&g)[8]) {
-  if (a.gain_f32) load8(static_cast<const float*>(a.gain) + c, valid, g);
-  else load8(static_cast<const uint16_t*>(a.gain) + c, valid, g);
-}
-
-// h of 8 elements: x, or x + residual rounded to the storage type and kept.
-template <typename T>
-__device__ __forceinline__ void load_h(const NormArgs& a, int64_t row, int64_t c, int64_t valid,
-                                       float (&h)[8]) {
-  const T* x = static_cast<const T*>(a.x);
-  load8(x + row * a.ld_x + c, valid, h);
-  if (a.residual != nullptr) {
-    float r[8];
-    load8(static_cast<const T*>(a.residual) + row * a.ld_residual + c, valid, r);
+template <typename Args>
+__device__ __forceinline__ void load_gain(const Args& a, int64_t c, float (&g)[8]) {
+  if (a.gain_f32) {
+    Vec8<float> v;
+    v.load(static_cast<const float*>(a.gain) + c, a.cols - c);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[j] = as_stored(x, h[j] + r[j]);
+    for (int j = 0; j < 8; ++j) g[j] = v[j];
+  } else {
+    Vec8<uint16_t> v;
+    v.load(static_cast<const uint16_t*>(a.gain) + c, a.cols - c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = v[j];
   }
 }
+
+// x + residual, rounded to the storage type.
 template <typename T>
-__device__ __forceinline__ void store_h(const NormArgs& a, int64_t row, int64_t c, int64_t valid,
-                                        const float (&h)[8]) {
-  if (a.h != nullptr) store8(static_cast<T*>(a.h) + row * a.ld_h + c, valid, h);
+__device__ __forceinline__ void add(Vec8<T>& x, const Vec8<T>& r) {
+  float s[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s[j] = x[j] + r[j];
+  x.set(s);
 }
 
 // y of 8 elements written, in its own type and in 8 bits.  Every lane of a
-// 16-lane group calls it (the group's largest magnitude is theirs).
+// 16-lane group calls it (the group's largest magnitude is theirs); elements
+// past the row's end are zeros.
 template <typename T>
-__device__ __forceinline__ void store_y(const NormArgs& a, int64_t row, int64_t c, int64_t valid,
-                                        const float (&h)[8], float rstd, const float (&g)[8]) {
-  float y[8];
+__device__ __forceinline__ void store_y(const NormArgs& a, int64_t row, int64_t c,
+                                        const Vec8<T>& h, float rstd) {
+  const int64_t valid = a.cols - c;
+  float g[8];
+  load_gain(a, c, g);
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    y[j] = as_stored(static_cast<const T*>(nullptr), (h[j] * rstd) * g[j]);
-  if (a.y != nullptr) store8(static_cast<T*>(a.y) + row * a.ld_y + c, valid, y);
+  for (int j = 0; j < 8; ++j) g[j] = j < valid ? (h[j] * rstd) * g[j] : 0.0f;
+  Vec8<T> y;
+  y.set(g);
+  if (a.y != nullptr) y.template store<true>(static_cast<T*>(a.y) + row * a.ld_y + c, valid);
   if (a.q.data != nullptr) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, j < valid ? abs_bits(y[j]) : 0u);
-    const uint32_t code = fp8_code(max16(m));
+    const uint32_t code = fp8_code(max16(abs_max(y)));
     store_bytes8(a.q.data + row * a.q.ld + c, valid, quant8(y, code));
     if ((threadIdx.x & 15) == 0 && valid > 0)
       a.q.scale[row * a.q.ld_scale + c / kFp8Group] = static_cast<uint8_t>(code);
   }
 }
 
-template <typename T, int NT, int V>
+// RES: a residual is added (and h written); without one h may still be wanted.
+template <typename T, int NT, int V, bool RES>
 __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
   __shared__ float red[2][NT / 64];
   int flip = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    float h[V][8];
+    Vec8<T> h[V], r[RES ? V : 1];
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8;
-      load_h<T>(a, row, c, a.cols - c, h[i]);
+      h[i].template load<true>(static_cast<const T*>(a.x) + row * a.ld_x + c, a.cols - c);
+      if constexpr (RES)
+        r[i].template load<true>(static_cast<const T*>(a.residual) + row * a.ld_residual + c,
+                                 a.cols - c);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8;
-      if (a.residual != nullptr || a.h != a.x) store_h<T>(a, row, c, a.cols - c, h[i]);
+      if constexpr (RES) add(h[i], r[i]);
+      if (RES || (a.h != nullptr && a.h != a.x))
+        h[i].template store<true>(static_cast<T*>(a.h) + row * a.ld_h + c, a.cols - c);
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss += h[i][j] * h[i][j];
     }
@@ -112,12 +115,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
     const float rstd = 1.0f / sqrtf(mean + a.eps);
     if (threadIdx.x == 0) a.rstd[row] = rstd;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int64_t c = (threadIdx.x + i * NT) * 8;
-      float g[8];
-      load_gain(a, c, a.cols - c, g);
-      store_y<T>(a, row, c, a.cols - c, h[i], rstd, g);
-    }
+    for (int i = 0; i < V; ++i) store_y(a, row, (threadIdx.x + i * NT) * 8, h[i], rstd);
   }
 }
 
@@ -127,9 +125,17 @@ __global__ __launch_bounds__(NT) void rmsnorm_wide_kernel(NormArgs a) {
   int flip = 0;
   const int64_t span = (a.cols + 8 * NT - 1) / (8 * NT) * (8 * NT);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    float ss = 0.0f, h[8], g[8];
+    Vec8<T> h, r;
+    const auto load_h = [&](int64_t c) {
+      h.load(static_cast<const T*>(a.x) + row * a.ld_x + c, a.cols - c);
+      if (a.residual != nullptr) {
+        r.load(static_cast<const T*>(a.residual) + row * a.ld_residual + c, a.cols - c);
+        add(h, r);
+      }
+    };
+    float ss = 0.0f;
     for (int64_t c = threadIdx.x * 8; c < a.cols; c += 8 * NT) {
-      load_h<T>(a, row, c, a.cols - c, h);
+      load_h(c);
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss += h[j] * h[j];
     }
@@ -138,11 +144,10 @@ __global__ __launch_bounds__(NT) void rmsnorm_wide_kernel(NormArgs a) {
     const float rstd = 1.0f / sqrtf(mean + a.eps);
     if (threadIdx.x == 0) a.rstd[row] = rstd;
     for (int64_t c = threadIdx.x * 8; c < span; c += 8 * NT) {
-      // (h may be x's or the residual's own buffer: read before it is written)
-      load_h<T>(a, row, c, a.cols - c, h);
-      if (a.residual != nullptr || a.h != a.x) store_h<T>(a, row, c, a.cols - c, h);
-      load_gain(a, c, a.cols - c, g);
-      store_y<T>(a, row, c, a.cols - c, h, rstd, g);
+      load_h(c);  // (before h, which may be x's or the residual's own buffer, is written)
+      if (a.residual != nullptr || (a.h != nullptr && a.h != a.x))
+        h.store(static_cast<T*>(a.h) + row * a.ld_h + c, a.cols - c);
+      store_y(a, row, c, h, rstd);
     }
   }
 }
@@ -154,42 +159,48 @@ __device__ __forceinline__ void block_rows(int64_t rows, int64_t blocks, int64_t
   r1 = rows * (b + 1) / blocks;
 }
 
-template <typename T, int NT, int V, bool DGAIN>
+// The next row is loaded while the present one is reduced.
+template <typename T, int NT, int V, bool DRES, bool DGAIN>
 __global__ __launch_bounds__(NT) void rmsnorm_backward_kernel(NormBwdArgs a) {
   __shared__ float red[2][NT / 64];
-  const T* dy = static_cast<const T*>(a.dy);
-  const T* h = static_cast<const T*>(a.h);
-  const T* dres = static_cast<const T*>(a.dres);
   float dg[V][8], g[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int64_t c = (threadIdx.x + i * NT) * 8;
-    load_gain(a, c, a.cols - c, g[i]);
+    load_gain(a, (threadIdx.x + i * NT) * 8, g[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) dg[i][j] = 0.0f;
   }
   int64_t r0, r1;
   block_rows(a.rows, gridDim.x, blockIdx.x, r0, r1);
-  int flip = 0;
-  for (int64_t row = r0; row < r1; ++row) {
-    const float rstd = a.rstd[row];
-    float d[V][8], hh[V][8], r[V][8];
-    float s = 0.0f;
+  struct Row {
+    Vec8<T> dy[V], h[V], dres[DRES ? V : 1];
+    float rstd;
+  };
+  const auto load_row = [&](Row& w, int64_t row) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int64_t c = (threadIdx.x + i * NT) * 8;
-      load8(dy + row * a.ld_dy + c, a.cols - c, d[i]);
-      load8(h + row * a.ld_h + c, a.cols - c, hh[i]);
-      if (dres != nullptr) load8(dres + row * a.ld_dres + c, a.cols - c, r[i]);
+      const int64_t c = (threadIdx.x + i * NT) * 8, valid = a.cols - c;
+      w.dy[i].load(static_cast<const T*>(a.dy) + row * a.ld_dy + c, valid);
+      w.h[i].load(static_cast<const T*>(a.h) + row * a.ld_h + c, valid);
+      if constexpr (DRES)
+        w.dres[i].load(static_cast<const T*>(a.dres) + row * a.ld_dres + c, valid);
     }
+    w.rstd = a.rstd[row];
+  };
+  Row next;
+  if (r0 < r1) load_row(next, r0);
+  int flip = 0;
+  for (int64_t row = r0; row < r1; ++row) {
+    const Row w = next;
+    if (row + 1 < r1) load_row(next, row + 1);
+    float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        hh[i][j] *= rstd;
-        if (DGAIN) dg[i][j] += d[i][j] * hh[i][j];
-        d[i][j] *= g[i][j];
-        s += d[i][j] * hh[i][j];
+        const float hh = w.h[i][j] * w.rstd;
+        if (DGAIN) dg[i][j] += w.dy[i][j] * hh;
+        s += (w.dy[i][j] * g[i][j]) * hh;
       }
     const float mean = block_sum<NT>(s, red[flip]) / static_cast<float>(a.cols);
     flip ^= 1;
@@ -199,17 +210,21 @@ __global__ __launch_bounds__(NT) void rmsnorm_backward_kernel(NormBwdArgs a) {
       float o[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        o[j] = rstd * (d[i][j] - hh[i][j] * mean);
-        if (dres != nullptr) o[j] += r[i][j];
+        o[j] = w.rstd * (w.dy[i][j] * g[i][j] - (w.h[i][j] * w.rstd) * mean);
+        if constexpr (DRES) o[j] += w.dres[i][j];
       }
-      store8(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.cols - c, o);
+      Vec8<T> out;
+      out.set(o);
+      out.template store<true>(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.cols - c);
     }
   }
   if constexpr (DGAIN) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8;
-      store8(a.part + blockIdx.x * a.cols + c, a.cols - c, dg[i]);
+      Vec8<float> out;
+      out.set(dg[i]);
+      out.store(a.part + blockIdx.x * a.cols + c, a.cols - c);
     }
   }
 }
@@ -222,102 +237,124 @@ __global__ __launch_bounds__(256) void rmsnorm_dgain_wide_kernel(NormBwdArgs a) 
   if (c >= a.cols) return;
   int64_t r0, r1;
   block_rows(a.rows, gridDim.y, blockIdx.y, r0, r1);
-  float dg[8] = {}, d[8], h[8];
+  float dg[8] = {};
   for (int64_t row = r0; row < r1; ++row) {
-    load8(static_cast<const T*>(a.dy) + row * a.ld_dy + c, a.cols - c, d);
-    load8(static_cast<const T*>(a.h) + row * a.ld_h + c, a.cols - c, h);
+    Vec8<T> d, h;
+    d.load(static_cast<const T*>(a.dy) + row * a.ld_dy + c, a.cols - c);
+    h.load(static_cast<const T*>(a.h) + row * a.ld_h + c, a.cols - c);
     const float rstd = a.rstd[row];
 #pragma unroll
     for (int j = 0; j < 8; ++j) dg[j] += d[j] * (h[j] * rstd);
   }
-  store8(a.part + blockIdx.y * a.cols + c, a.cols - c, dg);
+  Vec8<float> out;
+  out.set(dg);
+  out.store(a.part + blockIdx.y * a.cols + c, a.cols - c);
 }
 
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void rmsnorm_dx_wide_kernel(NormBwdArgs a) {
   __shared__ float red[2][NT / 64];
   int flip = 0;
-  float d[8], h[8], g[8], r[8];
+  Vec8<T> d, h, r;
+  float g[8];
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
     const T* hp = static_cast<const T*>(a.h) + row * a.ld_h;
     const float rstd = a.rstd[row];
     float s = 0.0f;
     for (int64_t c = threadIdx.x * 8; c < a.cols; c += 8 * NT) {
-      load8(dy + c, a.cols - c, d);
-      load8(hp + c, a.cols - c, h);
-      load_gain(a, c, a.cols - c, g);
+      d.load(dy + c, a.cols - c);
+      h.load(hp + c, a.cols - c);
+      load_gain(a, c, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s += (d[j] * g[j]) * (h[j] * rstd);
     }
     const float mean = block_sum<NT>(s, red[flip]) / static_cast<float>(a.cols);
     flip ^= 1;
     for (int64_t c = threadIdx.x * 8; c < a.cols; c += 8 * NT) {
-      load8(dy + c, a.cols - c, d);
-      load8(hp + c, a.cols - c, h);
-      load_gain(a, c, a.cols - c, g);
+      d.load(dy + c, a.cols - c);
+      h.load(hp + c, a.cols - c);
+      load_gain(a, c, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) d[j] = rstd * (d[j] * g[j] - (h[j] * rstd) * mean);
+      for (int j = 0; j < 8; ++j) g[j] = rstd * (d[j] * g[j] - (h[j] * rstd) * mean);
       if (a.dres != nullptr) {
-        load8(static_cast<const T*>(a.dres) + row * a.ld_dres + c, a.cols - c, r);
+        r.load(static_cast<const T*>(a.dres) + row * a.ld_dres + c, a.cols - c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] += r[j];
+        for (int j = 0; j < 8; ++j) g[j] += r[j];
       }
-      store8(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.cols - c, d);
+      d.set(g);
+      d.store(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.cols - c);
     }
   }
 }
 
-// dgain[j] = the sum of column j's `parts` partials, each of 4 waves a
-// contiguous share of them in order, then the waves in order.
-__global__ __launch_bounds__(256) void dgain_kernel(const float* __restrict__ part, int64_t parts,
-                                                    int64_t cols, float* __restrict__ dgain) {
-  __shared__ float red[4][64];
+// dgain[j] = the sum of column j's `parts` partials: each of 16 waves a
+// contiguous share of them in order, eight loads in flight, then the waves in
+// order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void dgain_kernel(const float* __restrict__ part,
+                                                                int64_t parts, int64_t cols,
+                                                                float* __restrict__ dgain) {
+  __shared__ float red[kJoinWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
-  const int64_t p0 = parts * wave / 4, p1 = parts * (wave + 1) / 4;
+  const int64_t p1 = parts * (wave + 1) / kJoinWaves;
   float s = 0.0f;
   if (c < cols)
-    for (int64_t p = p0; p < p1; ++p) s += part[p * cols + c];
+    for (int64_t p = parts * wave / kJoinWaves; p < p1; p += 8) {
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = p + q < p1 ? part[(p + q) * cols + c] : 0.0f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s += v[q];
+    }
   red[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && c < cols) dgain[c] = ((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane];
+  if (wave != 0 || c >= cols) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWaves; ++w) s += red[w][lane];
+  dgain[c] = s;
 }
 
 constexpr int64_t kMaxGrid = int64_t(1) << 22;
-constexpr int64_t kWideCols = 1024 * 8 * 4;  // the widest row kept in registers
+constexpr int64_t kWideCols = 1024 * 8 * 2;  // the widest row kept in registers
 
-// Blocks of the backward pass (partial sums of the gain's gradient).
-int64_t backward_blocks(int64_t rows) { return rows < 512 ? rows : 512; }
+// Threads of a backward block, and blocks (partial sums of the gain's gradient):
+// what the CUs hold at once, 2048 threads each, up to 8 blocks a CU.
+int backward_threads(int64_t cols) {
+  return cols <= 512 ? 64 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024;
+}
+int64_t backward_blocks(int64_t rows, int64_t cols) {
+  return std::min<int64_t>(rows, std::min(2048, (256 * 2048) / backward_threads(cols)));
+}
 
-template <typename T>
+template <typename T, bool RES>
 void norm_forward(const NormArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(a.rows < kMaxGrid ? a.rows : kMaxGrid));
 #define ZF_NORM(NT, V) \
-  hipLaunchKernelGGL((rmsnorm_kernel<T, NT, V>), grid, dim3(NT), 0, s, a)
+  hipLaunchKernelGGL((rmsnorm_kernel<T, NT, V, RES>), grid, dim3(NT), 0, s, a)
   if (a.cols <= 512) ZF_NORM(64, 1);
   else if (a.cols <= 2048) ZF_NORM(256, 1);
   else if (a.cols <= 4096) ZF_NORM(256, 2);
-  else if (a.cols <= 8192) ZF_NORM(256, 4);
-  else if (a.cols <= 16384) ZF_NORM(1024, 2);
-  else if (a.cols <= kWideCols) ZF_NORM(1024, 4);
+  else if (a.cols <= 8192) ZF_NORM(512, 2);
+  else if (a.cols <= kWideCols) ZF_NORM(1024, 2);
   else hipLaunchKernelGGL((rmsnorm_wide_kernel<T, 1024>), grid, dim3(1024), 0, s, a);
 #undef ZF_NORM
 }
 
-template <typename T, bool DGAIN>
+template <typename T, bool DRES, bool DGAIN>
 void norm_backward(const NormBwdArgs& a, hipStream_t s) {
   const int64_t blocks =
-      DGAIN ? backward_blocks(a.rows) : (a.rows < kMaxGrid ? a.rows : kMaxGrid);
+      DGAIN ? backward_blocks(a.rows, a.cols) : (a.rows < kMaxGrid ? a.rows : kMaxGrid);
   const dim3 grid(static_cast<uint32_t>(blocks));
 #define ZF_NORM(NT, V) \
-  hipLaunchKernelGGL((rmsnorm_backward_kernel<T, NT, V, DGAIN>), grid, dim3(NT), 0, s, a)
-  if (a.cols <= 512) ZF_NORM(64, 1);
-  else if (a.cols <= 2048) ZF_NORM(256, 1);
-  else if (a.cols <= 4096) ZF_NORM(512, 1);
+  hipLaunchKernelGGL((rmsnorm_backward_kernel<T, NT, V, DRES, DGAIN>), grid, dim3(NT), 0, s, a)
+  const int nt = backward_threads(a.cols);
+  if (nt == 64) ZF_NORM(64, 1);
+  else if (nt == 256) ZF_NORM(256, 1);
+  else if (nt == 512) ZF_NORM(512, 1);
   else if (a.cols <= 8192) ZF_NORM(1024, 1);
-  else if (a.cols <= 16384) ZF_NORM(1024, 2);
-  else if (a.cols <= kWideCols) ZF_NORM(1024, 4);
+  else if (a.cols <= kWideCols) ZF_NORM(1024, 2);
   else {
     if (DGAIN)
       hipLaunchKernelGGL((rmsnorm_dgain_wide_kernel<T>),
@@ -331,33 +368,44 @@ void norm_backward(const NormBwdArgs& a, hipStream_t s) {
 #undef ZF_NORM
 }
 
+template <typename T>
+void norm_backward(const NormBwdArgs& a, hipStream_t s) {
+  if (a.dres != nullptr) {
+    if (a.dgain != nullptr) norm_backward<T, true, true>(a, s);
+    else norm_backward<T, true, false>(a, s);
+  } else {
+    if (a.dgain != nullptr) norm_backward<T, false, true>(a, s);
+    else norm_backward<T, false, false>(a, s);
+  }
+}
+
 }  // namespace
 
 hipError_t launch_rmsnorm(const NormArgs& a, int32_t dtype, hipStream_t s) {
   (void)hipGetLastError();
-  if (dtype == ZF_BF16) norm_forward<uint16_t>(a, s);
-  else norm_forward<float>(a, s);
+  if (dtype == ZF_BF16) {
+    if (a.residual != nullptr) norm_forward<uint16_t, true>(a, s);
+    else norm_forward<uint16_t, false>(a, s);
+  } else {
+    if (a.residual != nullptr) norm_forward<float, true>(a, s);
+    else norm_forward<float, false>(a, s);
+  }
   return hipGetLastError();
 }
 
 size_t rmsnorm_backward_workspace(int64_t rows, int64_t cols) {
-  return static_cast<size_t>(backward_blocks(rows)) * static_cast<size_t>(cols) * sizeof(float);
+  return static_cast<size_t>(backward_blocks(rows, cols)) * static_cast<size_t>(cols) * sizeof(float);
 }
 
 hipError_t launch_rmsnorm_backward(const NormBwdArgs& a, int32_t dtype, hipStream_t s) {
   (void)hipGetLastError();
   if (a.rows > 0) {
-    if (dtype == ZF_BF16) {
-      if (a.dgain != nullptr) norm_backward<uint16_t, true>(a, s);
-      else norm_backward<uint16_t, false>(a, s);
-    } else {
-      if (a.dgain != nullptr) norm_backward<float, true>(a, s);
-      else norm_backward<float, false>(a, s);
-    }
+    if (dtype == ZF_BF16) norm_backward<uint16_t>(a, s);
+    else norm_backward<float>(a, s);
   }
   if (a.dgain != nullptr)  // (no rows: no partials, zeros)
-    hipLaunchKernelGGL(dgain_kernel, dim3(static_cast<uint32_t>((a.cols + 63) / 64)), dim3(256), 0,
-                       s, a.part, backward_blocks(a.rows), a.cols, a.dgain);
+    hipLaunchKernelGGL(dgain_kernel, dim3(static_cast<uint32_t>((a.cols + 63) / 64)),
+                       dim3(64 * kJoinWaves), 0, s, a.part, backward_blocks(a.rows, a.cols), a.cols, a.dgain);
   return hipGetLastError();
 }
 

@@ -63,10 +63,10 @@ class Fp8:
         data, scale, group = self.data, self.scale, self.group
         if group not in (1, 128):
             raise ValueError(f"{name}: group is 1 or 128, got {group}")
+        ld = _mat(data, DATA, name, rows, cols)
         r, c = data.shape
         sr, sc = -(-r // group), -(-c // 128)
-        ld = _mat(data, DATA, name, rows, cols)
-        ld_scale = _mat(scale, SCALE, f"{name}.scale", sr, sc)
+        ld_scale = _mat(scale, SCALE, name, sr, sc)
         if r <= 1 or not c:  # (a single row's stride is its width, as in _mat)
             ld = _up(c, 16)
         if sr <= 1 or not c:
@@ -76,25 +76,38 @@ class Fp8:
                 raise ValueError(f"{name}: row strides must be multiples of 16 (data) and 4 "
                                  f"(scale), got {ld} and {ld_scale}")
             # rows are read in whole units of 16 bytes, their scales of 4
-            for t, n, w in ((data, r, _up(c, 16)), (scale, sr, _up(sc, 4))):
-                step = t.stride(0) if n > 1 else 0
-                if t.untyped_storage().nbytes() < t.storage_offset() + (n - 1) * step + w:
-                    raise ValueError(f"{name}: the last row's storage ends inside a unit "
-                                     f"(alloc_fp8 pads rows)")
-        return ZfFp8(_ptr(data), ld, _ptr(scale), ld_scale, group)
+            if c % 16:
+                self._room(name, data, ld, _up(c, 16))
+            if sc % 4:
+                self._room(name, scale, ld_scale, _up(sc, 4))
+        return ZfFp8(data.data_ptr() or None, ld, scale.data_ptr() or None, ld_scale, group)
+
+    @staticmethod
+    def _room(name: str, t: torch.Tensor, ld: int, width: int) -> None:
+        end = t.storage_offset() + (t.shape[0] - 1) * ld + width
+        if t.untyped_storage().nbytes() < end:
+            raise ValueError(f"{name}: the last row's storage ends inside a unit (alloc_fp8 pads "
+                             f"rows)")
+
+
+def _alloc_fp8(rows: int, cols: int, group: int, device) -> Tuple[Fp8, ZfFp8]:
+    """A new Fp8 and its C struct."""
+    sr, sc = -(-rows // group), -(-cols // 128)
+    ld, ld_scale = _up(cols, 16), _up(sc, 4)
+    data = torch.empty((rows, ld), dtype=DATA, device=device)
+    scale = torch.empty((sr, ld_scale), dtype=SCALE, device=device)
+    c = ZfFp8(data.data_ptr() or None, ld, scale.data_ptr() or None, ld_scale, group)
+    if ld != cols:
+        data = data[:, :cols]
+    if ld_scale != sc:
+        scale = scale[:, :sc]
+    return Fp8(data, scale, group), c
 
 
 def alloc_fp8(rows: int, cols: int, group: int = 1, device="cuda") -> Fp8:
     """Uninitialised storage of a rows x cols matrix in 8 bits, rows padded to
     multiples of 16 bytes (data) and 4 (scale)."""
-    sr, sc = -(-rows // group), -(-cols // 128)
-    data = torch.empty((rows, _up(cols, 16)), dtype=DATA, device=device)
-    scale = torch.empty((sr, _up(sc, 4)), dtype=SCALE, device=device)
-    if data.shape[1] != cols:
-        data = data[:, :cols]
-    if scale.shape[1] != sc:
-        scale = scale[:, :sc]
-    return Fp8(data, scale, group)
+    return _alloc_fp8(rows, cols, group, device)[0]
 
 
 def quantize_fp8(x: torch.Tensor, group: int = 1, rows: bool = True, transposed: bool = False,
@@ -105,14 +118,17 @@ def quantize_fp8(x: torch.Tensor, group: int = 1, rows: bool = True, transposed:
     dt = _dtype(x, "x")
     ld = _mat(x, x.dtype, "x")
     r, c = x.shape
-    if out is None and rows:
-        out = alloc_fp8(r, c, group, x.device)
-    if out_t is None and transposed:
-        out_t = alloc_fp8(c, r, group, x.device)
+    c_out = c_out_t = None
+    if out is not None:
+        c_out = out.as_c("out", r, c)
+    elif rows:
+        out, c_out = _alloc_fp8(r, c, group, x.device)
+    if out_t is not None:
+        c_out_t = out_t.as_c("out_t", c, r)
+    elif transposed:
+        out_t, c_out_t = _alloc_fp8(c, r, group, x.device)
     if out is None and out_t is None:
         raise ValueError("neither output is wanted")
-    c_out = out.as_c("out", r, c) if out is not None else None
-    c_out_t = out_t.as_c("out_t", c, r) if out_t is not None else None
     _check("zf_quantize_fp8", LIB.zf_quantize_fp8(
         _ptr(x), dt, r, c, ld, ctypes.byref(c_out) if c_out is not None else None,
         ctypes.byref(c_out_t) if c_out_t is not None else None, _stream(stream)))
@@ -134,9 +150,10 @@ def matmul_fp8(a: Fp8, b: Fp8, out: Optional[torch.Tensor] = None, dtype=torch.b
     n = b.data.shape[0]
     c_a, c_b = a.as_c("a"), b.as_c("b", None, k)
     if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=a.data.device)
+        out, ld = torch.empty((m, n), dtype=dtype, device=a.data.device), n
+    else:
+        ld = _mat(out, out.dtype, "out", m, n)
     dt = _dtype(out, "out")
-    ld = _mat(out, out.dtype, "out", m, n)
     need = LIB.zf_matmul_fp8_workspace_bytes(m, n, k)
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
@@ -172,23 +189,26 @@ def rmsnorm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tensor
     r, c = x.shape
     gdt = _dtype(gain, "gain")
     _vec(gain, gain.dtype, "gain", c)
+    dtype, dev = x.dtype, x.device
     if rstd is None:
-        rstd = torch.empty(r, dtype=torch.float32, device=x.device)
-    _vec(rstd, torch.float32, "rstd", r)
-    ld_res = ld_h = ld_y = 0
+        rstd = torch.empty(r, dtype=torch.float32, device=dev)
+    else:
+        _vec(rstd, torch.float32, "rstd", r)
+    ld_res, ld_h, ld_y, c_q = 0, c, c, None
     if residual is not None:
-        ld_res = _mat(residual, x.dtype, "residual", r, c)
-        if h is None:
-            h = torch.empty((r, c), dtype=x.dtype, device=x.device)
+        ld_res = _mat(residual, dtype, "residual", r, c)
     if h is not None:
-        ld_h = _mat(h, x.dtype, "h", r, c)
-    if y is None and want_y:
-        y = torch.empty((r, c), dtype=x.dtype, device=x.device)
+        ld_h = _mat(h, dtype, "h", r, c)
+    elif residual is not None:
+        h = torch.empty((r, c), dtype=dtype, device=dev)
     if y is not None:
-        ld_y = _mat(y, x.dtype, "y", r, c)
-    if q is None and want_q:
-        q = alloc_fp8(r, c, 1, x.device)
-    c_q = q.as_c("q", r, c) if q is not None else None
+        ld_y = _mat(y, dtype, "y", r, c)
+    elif want_y:
+        y = torch.empty((r, c), dtype=dtype, device=dev)
+    if q is not None:
+        c_q = q.as_c("q", r, c)
+    elif want_q:
+        q, c_q = _alloc_fp8(r, c, 1, dev)
     _check("zf_rmsnorm_forward", LIB.zf_rmsnorm_forward(
         _ptr(x), ld, _ptr(residual), ld_res, dt, r, c, _ptr(gain), gdt, float(eps), _ptr(h), ld_h,
         _ptr(y), ld_y, ctypes.byref(c_q) if c_q is not None else None, _ptr(rstd),
@@ -220,12 +240,14 @@ def rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd
     if dresidual is not None:
         ld_res = _mat(dresidual, dy.dtype, "dresidual", r, c)
     if dx is None:
-        dx = torch.empty((r, c), dtype=dy.dtype, device=dy.device)
-    ld_dx = _mat(dx, dy.dtype, "dx", r, c)
-    if dgain is None and want_dgain:
-        dgain = torch.empty(c, dtype=torch.float32, device=dy.device)
+        dx, ld_dx = torch.empty((r, c), dtype=dy.dtype, device=dy.device), c
+    else:
+        ld_dx = _mat(dx, dy.dtype, "dx", r, c)
     if dgain is not None:
         _vec(dgain, torch.float32, "dgain", c)
+    elif want_dgain:
+        dgain = torch.empty(c, dtype=torch.float32, device=dy.device)
+    if dgain is not None:
         if workspace is None:
             need = LIB.zf_rmsnorm_backward_workspace_bytes(r, c)
             workspace = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
