@@ -194,6 +194,59 @@ def test_matmul_extreme_scales(m):
     product_check(a, b, a64 * 2.0 ** -127, b64 * 2.0 ** 120, torch.bfloat16)
 
 
+@pytest.mark.parametrize("m", [1, 300])
+@pytest.mark.parametrize("codes", [(20, 200), (110, 0), (240, 20)])
+def test_matmul_far_scales(m, codes):
+    """fp32 results with scales far from 1, the values within bf16's range: bound
+    as ever, plus what counts as zero (below 2^-126)."""
+    gen = torch.Generator().manual_seed(14)
+    a, a64 = R.random_fp8(zf, m, 256, 1, gen, spread=0)
+    b, b64 = R.random_fp8(zf, 64, 256, 1, gen, spread=0)
+    a.scale.view(torch.uint8).fill_(codes[0])
+    b.scale.view(torch.uint8).fill_(codes[1])
+    sa, sb = 2.0 ** (codes[0] - 127), 2.0 ** (codes[1] - 127)
+    got = zf.matmul_fp8(a, b, dtype=torch.float32).double().cpu()
+    want = (a64 @ b64.t()) * sa * sb
+    lost = 2.0 ** -126 * (a64.abs().sum(1)[:, None] * sa + b64.abs().sum(1)[None] * sb)
+    tol = 24 * 2.0 ** -23 * (a64.abs() @ b64.abs().t()) * sa * sb + lost
+    assert ((got - want).abs() <= tol).all()
+
+
+def test_graph_replays():
+    """Norm and product of a token captured once, replayed on new inputs between
+    eager work, every replay against the eager result."""
+    gen = torch.Generator().manual_seed(8)
+    x = torch.empty(3, 512, dtype=torch.bfloat16, device="cuda")
+    res = torch.empty_like(x)
+    g = torch.ones(512, dtype=torch.bfloat16, device="cuda")
+    w, _ = zf.quantize_fp8((torch.randn(700, 512, generator=gen) / 20).to(torch.bfloat16).cuda(), 128)
+    w300, _ = zf.quantize_fp8(torch.randn(256, 6000, generator=gen).to(torch.bfloat16).cuda(), 128)
+    wide = torch.randn(40, 6000, generator=gen).to(torch.bfloat16).cuda()  # a split reduction
+
+    def run():
+        n = zf.rmsnorm(x, g, res, want_y=False, want_q=True)
+        return n.h, zf.matmul_fp8(n.q, w), zf.matmul_fp8(zf.quantize_fp8(wide)[0], w300)
+
+    def fill():
+        for t in (x, res, wide):
+            t.copy_(torch.randn(t.shape, generator=gen).to(t.dtype))
+
+    fill()
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for _ in range(4):
+        fill()
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
 def test_other_stream():
     """Work on a stream of its own, ordered by it."""
     gen = torch.Generator().manual_seed(4)
