@@ -88,9 +88,10 @@ size_t zf_matmul_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k);
  * instruction's arithmetic: e4m3's own rounding of an element is up to 2^-4);
  * with an fp32 result products and sums are fp32, values of a or b (elements
  * times scales) below 2^-126 may count as zero and those past bf16's range as
- * infinities.  m, n < 2^30; k and, with more than
- * one row, both ld_data < 2^23; fewer than 2^24 tiles of 128 x 128.  ws: zf_matmul_fp8_workspace_bytes(m, n, k) bytes,
- * 16-byte aligned (may be NULL if that is 0), contents overwritten. */
+ * infinities.  m, n < 2^30; k and, with more than one row, the strides of data
+ * and scale < 2^23; fewer than 2^24 tiles of 128 x 128.  ws:
+ * zf_matmul_fp8_workspace_bytes(m, n, k) bytes, 16-byte aligned (may be NULL if
+ * that is 0), contents overwritten. */
 zf_status zf_matmul_fp8(const zf_fp8* a, const zf_fp8* b, int64_t m, int64_t n, int64_t k,
                         void* out, int32_t out_dtype, int64_t ld_out, void* ws, size_t ws_bytes,
                         zf_stream stream);

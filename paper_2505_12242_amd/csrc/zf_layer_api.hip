@@ -127,8 +127,9 @@ zf_status zf_matmul_fp8(const zf_fp8* a, const zf_fp8* b, int64_t m, int64_t n, 
   const Fp8Spans sa = fp8_spans(a, m, k, ok), sb = fp8_spans(b, n, k, ok);
   const Span so = span(out, m, n, ld_out, dtype_size(out_dtype), ok);
   // a tile's rows are addressed through 32-bit offsets
-  if (k >= kStrideLimit || (m > 1 && k > 0 && a->ld_data >= kStrideLimit) ||
-      (n > 1 && k > 0 && b->ld_data >= kStrideLimit))
+  if (k >= kStrideLimit ||
+      (m > 1 && k > 0 && (a->ld_data >= kStrideLimit || a->ld_scale >= kStrideLimit)) ||
+      (n > 1 && k > 0 && (b->ld_data >= kStrideLimit || b->ld_scale >= kStrideLimit)))
     ok = false;
   if (!ok || ceil_div(m, 128) * ceil_div(n, 128) >= kGridLimit) return ZF_EINVAL;
   const size_t need = zf_matmul_fp8_workspace_bytes(m, n, k);

@@ -2,7 +2,18 @@
 // the reduction (formulas and format in zf_layer.h).
 //
 // out[i][j] = sum over groups g of 2^(ca[i][g] + cb[j][g] - 254) * sum over
-// the group of a * b.
+// the group of a * b.  The scaled matrix instruction of gfx950 takes the codes
+// beside the operands, so nothing is rescaled between groups.
+//
+// Three forms.  Many rows: tiles of 256 x 256, 128 x 256 or 128 x 128
+// (matmul_tile_kernel), bound by what the chip's power lets the matrix units do
+// and by L2: 2.37-2.65 PFLOP/s at 8192 x 11008 x 4096, 8192 x 4096 x 11008 and
+// 4096 x 11008 x 8192, where the same kernel without its loads reaches 3.1 and
+// the instruction alone on constant data 4.6.  Few tiles: the reduction is split
+// over blocks and the shares' results joined in order (64 x 11008 x 4096: 17 us).
+// Up to 16 rows: the second operand's bytes are all that counts
+// (matmul_rows_kernel; 1 x 11008 x 4096: 45 MB in 9.9 us, 4.6 TB/s).
+#include <algorithm>
 #include <type_traits>
 
 #include "zf_layer.hpp"
@@ -91,11 +102,11 @@ __device__ __forceinline__ u32x4 clear_tail(u32x4 v, int valid) {
 }
 
 // Tile of block b in a grid of mt x nt.  Each XCD takes a contiguous range of
-// the order; within it 8 tile rows are walked together, so that the tiles an
+// the order; within it 4 tile rows are walked together, so that the tiles an
 // XCD works on at once share rows of both operands in its L2.
 __device__ __forceinline__ void tile_of(uint32_t b, uint32_t mt, uint32_t nt, uint32_t& mi,
                                         uint32_t& ni) {
-  constexpr uint32_t kRows = 8;
+  constexpr uint32_t kRows = 4;
   const uint32_t B = mt * nt, q = B / kXcds, r = B % kXcds, x = b % kXcds, i = b / kXcds;
   const uint32_t id = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + i;
   const uint32_t g = id / (kRows * nt), left = mt - g * kRows, h = left < kRows ? left : kRows;
@@ -138,7 +149,7 @@ __device__ __forceinline__ void wait_reads() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// A 256-thread block computes a BM x BN tile, each wave a quarter of it, from S
+// A 256-thread block computes a BM x BN tile, each wave a quarter of it, from two
 // slots of 128 elements of the reduction in LDS.  Each half of a step multiplies
 // 64 elements from registers while the next 64 are read from LDS.  Memory is
 // loaded straight to LDS, in whole 128-byte lines, spread evenly over the
@@ -146,7 +157,7 @@ __device__ __forceinline__ void wait_reads() {
 // memory pipeline holds up the products behind it.  Rows past an operand's end
 // repeat its last row (their results are not stored); the units past the
 // reduction's end repeat the row's last one and are cleared in LDS.
-template <int BM, int BN, int S, bool PRECISE, bool PART>
+template <int BM, int BN, bool PRECISE, bool PART>
 __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
   constexpr int kRows = BM + BN;
@@ -154,10 +165,11 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   constexpr int kParts = TM + TN;  // fragments of half a step; 64 rows of the tile each
   constexpr int kCodeUnits = (kRows + 255) / 256;  // of 64 rows' codes, per four steps
   constexpr int kLoads = 2 * kParts + 1;  // of a wave per step: 8 rows each, and a part of the codes
-  constexpr int kCodes = S * kSlot;       // a word (four steps) a row, two groups of steps
+  constexpr int kCodes = 2 * kSlot;       // a word (four steps) a row, two groups of steps
   // A step's 2 kParts groups of products.  Groups kOpen .. issue its loads.
   constexpr int kOpen = TM / 2, kOpenB = kParts / 2, kIssue = 2 * kParts - kOpen;
   static_assert(TM % 2 == 0 && TN % 2 == 0, "two fragments are read at a time");
+  static_assert((kOpenB - kOpen) * kLoads / kIssue <= 2 * TM, "rows of x alone until y's are read");
   __shared__ __align__(1024) uint8_t lds[kCodes + 2 * kRows * 4];
   const int t = threadIdx.x, lane = t & 63, wave = uniform_i32(t >> 6);
   const int wm = (wave & 1) * WM, wn = (wave >> 1) * WN;
@@ -209,7 +221,7 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   };
   // The last step's bytes past the reduction's end cleared, once it has landed.
   const auto clear_slot = [&](int slot) {
-    __syncthreads();
+    wait_loads<0>();
     for (int r = t; r < kRows; r += 256)
       for (int c = tail / 16; c < 8; ++c) {
         u32x4* const u = reinterpret_cast<u32x4*>(
@@ -257,9 +269,9 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   // Step kt, in 2 kParts groups of products, of its first half and then of its
   // second.  During the first half's groups its second half is read, two
   // fragments a group, x's first: when every wave has them, the slot's rows of
-  // x, then those of y, take step kt + S.  During the second half's groups step
+  // x, then those of y, take step kt + 2.  During the second half's groups step
   // kt + 1's first half is read, a fragment a group: its rows of x have landed
-  // at the half's start (behind them, y's and what later steps have issued may still
+  // at the half's start (behind them, y's and what kt + 2 has issued may still
   // be in flight), those of y where it reaches them.  Past the last step the
   // last one is loaded and read again, into a slot that nothing uses: the loop
   // has no branch.  The codes of the next four steps are loaded one part a step.
@@ -268,12 +280,9 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
 #pragma unroll
     for (int i = 0; i < kCodeUnits; ++i) load_codes(first >> 2, i);
     load_step(first, 0);
-#pragma unroll
-    for (int i = 1; i < S; ++i) {
-      load_step(min(first + i, steps - 1), i);
-      load_codes(min((first >> 2) + 1, last_group), 0);
-    }
-    wait_loads<(S - 1) * kLoads>();
+    load_step(min(first + 1, steps - 1), 1);
+    load_codes(min((first >> 2) + 1, last_group), 0);
+    wait_loads<kLoads>();
     if (tail && first + 1 == steps) clear_slot(0);
     read_codes(first, ca, cb);
 #pragma unroll
@@ -281,8 +290,8 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   }
   int slot = 0;
   for (int kt = first; kt < steps; ++kt) {
-    const int next = slot + 1 == S ? 0 : slot + 1, ahead = min(kt + S, steps - 1);
-    // loads [g kLoads / kIssue, (g + 1) kLoads / kIssue) of step kt + S
+    const int next = slot ^ 1, ahead = min(kt + 2, steps - 1);
+    // loads [g kLoads / kIssue, (g + 1) kLoads / kIssue) of step kt + 2
     const auto issue = [&](auto g) {
       if constexpr (g.value >= 0)
 #pragma unroll
@@ -303,8 +312,8 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
     });
     int na[TM], nb[TN];
     for_parts<kParts>([&](auto g) {
-      // loads of steps past kt + 1 issued before this group
-      constexpr int issued = (S - 2) * kLoads + (kParts + g.value - kOpen) * kLoads / kIssue;
+      // loads of step kt + 2 issued before this group
+      constexpr int issued = (kParts + g.value - kOpen) * kLoads / kIssue;
       if constexpr (g.value == 0) {
         wait_loads<kLoads - 2 * TM + issued>();
         if (tail && kt + 2 == steps) clear_slot(next);
@@ -322,14 +331,14 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
     for (int j = 0; j < TN; ++j) cb[j] = nb[j];
     slot = next;
   }
-  __syncthreads();
+  wait_loads<0>();  // nothing lands in LDS from here on
 
   // A lane holds 4 consecutive columns of a row at a time; through LDS, 32
   // rows of the wave's tile at a time, the rows become contiguous.
   typedef typename std::conditional<PRECISE || PART, float, uint16_t>::type Out;
   constexpr int kPer = 16 / sizeof(Out);             // elements of a 16-byte store
   constexpr int kPitch = WN + kPer;
-  static_assert(4 * 32 * kPitch * sizeof(Out) <= S * kSlot, "the waves' slabs fit the slots");
+  static_assert(4 * 32 * kPitch * sizeof(Out) <= 2 * kSlot, "the waves' slabs fit the slots");
   Out* const slab = reinterpret_cast<Out*>(lds) + wave * 32 * kPitch;
   Out* const out = static_cast<Out*>(p.out) + (PART ? blockIdx.y * p.m * p.ld_out : 0) +
                    (m0 + wm) * p.ld_out + n0 + wn;
@@ -357,7 +366,7 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
       for (int r = 0; r < 32; r += kStep) {
         const int rr = r + lane / kRun;
         const u32x4 v = *reinterpret_cast<const u32x4*>(slab + rr * kPitch + c);
-        *reinterpret_cast<u32x4_h*>(out + (32 * i + rr) * p.ld_out + c) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4_h*>(out + (32 * i + rr) * p.ld_out + c));
       }
     } else {
 #pragma unroll 1
@@ -494,8 +503,12 @@ int64_t tiles(const int64_t m, const int64_t n, int bm, int bn) {
   return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
 }
 
-// Shares of the reduction for 128 x 128 tiles that do not fill the 256 CUs.
-int shares(int64_t m, int64_t n, int64_t k) {
+// Shares of the reduction where 128 x 128 tiles do not fill the 256 CUs: the
+// number for which this estimate in us is least.  A step takes 0.42 us on a CU
+// of its own and 0.58 as one of two (precise 0.95 and 1.75); a share's partial
+// result is written and read at some 6 TB/s, the joining launch costs 3.  E.g.
+// 512 x 1024 x 11008: 1 share 41 us, 8 shares 20.6; 256 x 4096 x 4096 18.1, 17.1.
+int shares(int64_t m, int64_t n, int64_t k, bool precise) {
   if (m <= kRowsMax) return 1;
   const int64_t t = tiles(m, n, 128, 128), steps = (k + kBK - 1) / kBK;
   if (t > 160) return 1;
@@ -503,9 +516,9 @@ int shares(int64_t m, int64_t n, int64_t k) {
   double least = 1e30;
   for (int s = 1; s <= 16 && s * t <= 512; ++s) {
     const int64_t per = ((steps + s - 1) / s + 3) / 4 * 4;  // (codes come four steps at a time)
-    if ((s - 1) * per >= steps && s > 1) continue;
-    const double us = static_cast<double>(per) * (s * t > 256 ? 0.58 : 0.42) +
-                      (s > 1 ? 3.0 + 8.0 * s * m * n / 6e6 : 0.0);
+    if (s > 1 && (s - 1) * per >= steps) continue;
+    const double step = s * t > 256 ? (precise ? 1.75 : 0.58) : (precise ? 0.95 : 0.42);
+    const double us = per * step + (s > 1 ? 3.0 + 8.0 * s * m * n / 6e6 : 0.0);
     if (us < least) {
       least = us;
       best = s;
@@ -528,20 +541,32 @@ void launch_rows(const MatmulArgs& a, hipStream_t s) {
 
 template <bool PRECISE>
 void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
-#define ZF_TILES(BM, BN, S, PART, Y, ARGS)                                                       \
-  hipLaunchKernelGGL((matmul_tile_kernel<BM, BN, S, PRECISE, PART>),                             \
+#define ZF_TILES(BM, BN, PART, Y, ARGS)                                                          \
+  hipLaunchKernelGGL((matmul_tile_kernel<BM, BN, PRECISE, PART>),                                \
                      dim3(static_cast<uint32_t>(tiles(a.m, a.n, BM, BN)), Y), dim3(256), 0, s, ARGS)
-  if (!PRECISE && tiles(a.m, a.n, 256, 256) >= 160) {
-    if constexpr (!PRECISE) ZF_TILES(256, 256, 2, false, 1, a);
-  } else if (tiles(a.m, a.n, 128, 256) >= 160) {
-    ZF_TILES(128, 256, 2, false, 1, a);
-  } else if (const int q = shares(a.m, a.n, a.k); q > 1) {
+  // Larger tiles ask less of the memory system and take longer to fill the
+  // chip.  Us with 256 x 256 / 128 x 256 / 128 x 128 tiles: 8192 x 4096 x 11008 285 /
+  // 352 / 402, 1024 x 11008 x 4096 (172 / 344 / 688 tiles) 49 / 58 / 52, 2048 x
+  // 4096 x 11008 (128 / 256 / 512) 118 / 92 / 104, 1024 x 4096 x 4096 (64 / 128 /
+  // 256) 44 / 29 / 24.  The precise form is bound by its products: 128 x 256 and
+  // 128 x 128 within 2% from 2048 x 4096 x 4096 on, 48 / 45 at 1003 x 5003 x 3001.
+  if constexpr (!PRECISE) {
+    if (tiles(a.m, a.n, 256, 256) >= 160) {
+      ZF_TILES(256, 256, false, 1, a);
+      return;
+    }
+    if (tiles(a.m, a.n, 128, 256) >= 160) {
+      ZF_TILES(128, 256, false, 1, a);
+      return;
+    }
+  }
+  if (const int q = shares(a.m, a.n, a.k, PRECISE); q > 1) {
     MatmulArgs b = a;
     b.out = ws;
     b.ld_out = a.n;
     const int64_t steps = (a.k + kBK - 1) / kBK;
     b.share = static_cast<int32_t>(((steps + q - 1) / q + 3) / 4 * 4);
-    ZF_TILES(128, 128, 2, true, q, b);
+    ZF_TILES(128, 128, true, q, b);
     const int64_t blocks = (a.m * a.n + 2047) / 2048;
     const dim3 grid(static_cast<uint32_t>(blocks < 2048 ? blocks : 2048));
     if (PRECISE)
@@ -553,7 +578,7 @@ void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
                          static_cast<const float*>(ws), q, a.m, a.n, static_cast<uint16_t*>(a.out),
                          a.ld_out);
   } else {
-    ZF_TILES(128, 128, 2, false, 1, a);
+    ZF_TILES(128, 128, false, 1, a);
   }
 #undef ZF_TILES
 }
@@ -561,7 +586,7 @@ void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
 }  // namespace
 
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k) {
-  const int q = shares(m, n, k);
+  const int q = std::max(shares(m, n, k, false), shares(m, n, k, true));
   return q > 1 ? static_cast<size_t>(q) * m * n * sizeof(float) : 0;
 }
 

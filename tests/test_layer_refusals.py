@@ -59,6 +59,7 @@ def test_matmul():
                dict(ld=59), dict(out=None), dict(out=addr(9) + 1), dict(dt=1, out=addr(9) + 2),
                dict(a=fp8(1, 192, 4)), dict(a=fp8(1, 200, 4)), dict(b=fp8(3, 208, 2)),
                dict(b=fp8(3, 208, 4, 2)), dict(a=fp8(1, 1 << 23, 4)), dict(b=fp8(3, 1 << 24, 4)),
+               dict(a=fp8(1, 208, 1 << 23)), dict(b=fp8(3, 208, 1 << 23)),
                dict(a=_lib.ZfFp8(None, 208, addr(2), 4, 1)), dict(out=addr(1)), dict(out=addr(4)),
                dict(m=1 << 29, n=1 << 29)):
         if kw.get("n") == 1 << 30 or kw.get("n") == 1 << 29:
