@@ -94,8 +94,7 @@ struct AdamTensor {
   int32_t grad_f32;
   int32_t pad;
 };
-constexpr int kAdamwChunk8 = 2048;  // elements per block, states in 8 bits
-constexpr int kAdamwChunk32 = 1024;  // and in 32
+constexpr int kAdamwChunk = 1024;  // elements per block
 hipError_t launch_adamw(const AdamTensor* tensors, const int64_t* off, int32_t count,
                         int64_t blocks, const AdamK& c, const float* grad_scale, hipStream_t s);
 

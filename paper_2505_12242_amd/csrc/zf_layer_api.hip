@@ -246,7 +246,7 @@ size_t adamw_bytes(int32_t count) {
 }
 
 int64_t adamw_chunks(const zf_adamw_tensor& t) {
-  return ceil_div(t.n, t.exp_avg_scale != nullptr ? zf::kAdamwChunk8 : zf::kAdamwChunk32);
+  return ceil_div(t.n, zf::kAdamwChunk);
 }
 
 bool adamw_tensor_ok(const zf_adamw_tensor& t) {
@@ -254,7 +254,7 @@ bool adamw_tensor_ok(const zf_adamw_tensor& t) {
   const bool eight = t.exp_avg_scale != nullptr;
   if (eight != (t.exp_avg_sq_scale != nullptr) && t.n > 0) return false;
   if (t.n == 0) return true;
-  if (t.n >= kGridLimit * zf::kAdamwChunk32) return false;
+  if (t.n >= kGridLimit * zf::kAdamwChunk) return false;
   const size_t state = eight ? 1 : 4;
   return t.grad != nullptr && aligned(t.grad, dtype_size(t.grad_dtype)) && t.master != nullptr &&
          aligned(t.master, 4) && aligned(t.weight, 2) && t.exp_avg != nullptr &&
