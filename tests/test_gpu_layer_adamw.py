@@ -181,3 +181,25 @@ def test_fresh_states_against_64_bits():
     # each step's relative error: 1/16 per stored moment and step, most of it forgotten
     rms = ((got[8] - p).square().mean() / moved.square().mean()).sqrt()
     assert rms < 0.1, rms
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("low,high", [(-62, -38), (38, 62)])
+def test_second_moments_at_the_ends_of_the_range(bits, low, high):
+    """Second moments on both sides of 2^-96 and of 2^100, in the same lanes and
+    in lanes of their own, up to where a square leaves fp32's range."""
+    t = Tensor(2053, bits, torch.float32, 0, 3, values="normal")
+    gen = torch.Generator().manual_seed(low)
+    e = torch.randint(low, high, (t.n,), generator=gen)
+    e[512:1536] = torch.arange(low, high).repeat_interleave(128)[:1024]
+    g = torch.ldexp(1 + torch.rand(t.n, generator=gen), e)
+    t.b.grad.copy_(g)
+    t.g = g.numpy()
+    plan = zf.AdamWPlan([t.b])
+    hp = zf.AdamHparams(lr=1e-3)
+    for step in (1, 2):
+        plan.step(hp, step)
+        torch.cuda.synchronize()
+        t.step(hp, step, None)
+        t.check()
+    plan.close()
