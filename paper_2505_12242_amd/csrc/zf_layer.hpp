@@ -115,32 +115,55 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // Eight elements as they are stored: loaded and stored with as few accesses as
 // any element alignment allows, widened where they are used.  Elements at and
 // past `valid` are zeros, neither read nor written.  NT: read or written once.
+//
+// A row's last, partial piece is read as 4, 2 and 1 elements, as the bits of
+// `valid` say, and put in order by settle(), which is where they are waited for:
+// load() is fetch() and settle().  (Element by element, each load waited for the
+// one before: 8192 rows of 5004 bf16 columns took 91 us, of 5120 columns 62.)
 template <typename T>
 struct Vec8;
 
+typedef uint32_t u32_h __attribute__((aligned(2)));
+typedef u32x2 u32x2_f __attribute__((aligned(4)));
 template <>
 struct Vec8<uint16_t> {
   u32x4 u;
   template <bool NT = false>
-  __device__ __forceinline__ void load(const uint16_t* p, int64_t valid) {
+  __device__ __forceinline__ void fetch(const uint16_t* p, int64_t valid) {
     if (valid >= 8) {
       u = NT ? load8_bf16(p) : *reinterpret_cast<const u32x4_h*>(p);
     } else {
       u = u32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < valid) u[j >> 1] |= static_cast<uint32_t>(p[j]) << (16 * (j & 1));
+      if (valid <= 0) return;
+      if (valid & 4) {
+        const u32x2 t = *reinterpret_cast<const u32x2_h*>(p);
+        u.x = t.x;
+        u.y = t.y;
+      }
+      if (valid & 2) u.z = *reinterpret_cast<const u32_h*>(p + (valid & 4));
+      if (valid & 1) u.w = p[valid - 1];
     }
+  }
+  __device__ __forceinline__ void settle(int64_t valid) {
+    if (valid >= 8) return;
+    const uint32_t t0 = valid & 2 ? u.z : u.w, t1 = valid & 2 ? u.w : 0u;
+    u = valid & 4 ? u32x4{u.x, u.y, t0, t1} : u32x4{t0, t1, 0u, 0u};
+  }
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const uint16_t* p, int64_t valid) {
+    fetch<NT>(p, valid);
+    settle(valid);
   }
   template <bool NT = false>
   __device__ __forceinline__ void store(uint16_t* p, int64_t valid) const {
     if (valid >= 8) {
       if (NT) store8_bf16(p, u);
       else *reinterpret_cast<u32x4_h*>(p) = u;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < valid) p[j] = static_cast<uint16_t>(u[j >> 1] >> (16 * (j & 1)));
+    } else if (valid > 0) {
+      if (valid & 4) *reinterpret_cast<u32x2_h*>(p) = u32x2{u.x, u.y};
+      const uint32_t t0 = valid & 4 ? u.z : u.x, t1 = valid & 4 ? u.w : u.y;
+      if (valid & 2) *reinterpret_cast<u32_h*>(p + (valid & 4)) = t0;
+      if (valid & 1) p[valid - 1] = static_cast<uint16_t>(valid & 2 ? t1 : t0);
     }
   }
   __device__ __forceinline__ float operator[](int j) const {
@@ -156,7 +179,7 @@ template <>
 struct Vec8<float> {
   u32x4 u[2];
   template <bool NT = false>
-  __device__ __forceinline__ void load(const float* p, int64_t valid) {
+  __device__ __forceinline__ void fetch(const float* p, int64_t valid) {
     if (valid >= 8) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -164,9 +187,32 @@ struct Vec8<float> {
         u[i] = NT ? __builtin_nontemporal_load(q) : *q;
       }
     } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) u[j >> 2][j & 3] = j < valid ? __float_as_uint(p[j]) : 0u;
+      u[0] = u[1] = u32x4{0, 0, 0, 0};
+      if (valid <= 0) return;
+      if (valid & 4) u[0] = *reinterpret_cast<const u32x4_f*>(p);
+      if (valid & 2) {
+        const u32x2 t = *reinterpret_cast<const u32x2_f*>(p + (valid & 4));
+        u[1].x = t.x;
+        u[1].y = t.y;
+      }
+      if (valid & 1) u[1].z = __float_as_uint(p[valid - 1]);
     }
+  }
+  __device__ __forceinline__ void settle(int64_t valid) {
+    if (valid >= 8) return;
+    const bool four = (valid & 4) != 0, two = (valid & 2) != 0;
+    const uint32_t t[4] = {two ? u[1].x : u[1].z, two ? u[1].y : 0u, two ? u[1].z : 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {  // (element by element: whole vectors go through memory)
+      const uint32_t a = u[0][j];
+      u[0][j] = four ? a : t[j];
+      u[1][j] = four ? t[j] : 0u;
+    }
+  }
+  template <bool NT = false>
+  __device__ __forceinline__ void load(const float* p, int64_t valid) {
+    fetch<NT>(p, valid);
+    settle(valid);
   }
   template <bool NT = false>
   __device__ __forceinline__ void store(float* p, int64_t valid) const {
@@ -177,10 +223,13 @@ struct Vec8<float> {
         if (NT) __builtin_nontemporal_store(u[i], q);
         else *q = u[i];
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < valid) p[j] = __uint_as_float(u[j >> 2][j & 3]);
+    } else if (valid > 0) {
+      if (valid & 4) *reinterpret_cast<u32x4_f*>(p) = u[0];
+      const bool four = (valid & 4) != 0;
+      const uint32_t t0 = four ? u[1].x : u[0].x, t1 = four ? u[1].y : u[0].y,
+                     t2 = four ? u[1].z : u[0].z;
+      if (valid & 2) *reinterpret_cast<u32x2_f*>(p + (valid & 4)) = u32x2{t0, t1};
+      if (valid & 1) p[valid - 1] = __uint_as_float(valid & 2 ? t2 : t0);
     }
   }
   __device__ __forceinline__ float operator[](int j) const {

@@ -3,10 +3,16 @@
 //
 // One block per row, the row in registers between its two uses: every input is
 // read once and every output written once.  A thread holds V pieces of 8
-// consecutive elements, NT * 8 elements apart; 16 lanes hold one group of the
-// 8-bit output.  Sums are fp32: per thread in order, then over the wave, then
-// over the block's waves.  Rows too wide for the registers are read twice
-// (the *_wide kernels).  Bound by HBM.
+// consecutive elements, NT * 8 elements apart, NT the fewest threads that hold
+// the row; 16 lanes hold one group of the 8-bit output.  Sums are fp32: per
+// thread in order, then over the wave, then over the block's waves.  Rows too
+// wide for the registers are read twice (the *_wide kernels).
+//
+// Bound by HBM.  8192 x 4096 bf16 with residual: forward 46 us (5.8 TB/s) with
+// one output, 50 us (6.0 TB/s) with both, backward 53 us (5.1 TB/s) and 5 us for
+// the gain's join; one row of 4096, 3.6 us, is latency.  Blocks of fewest
+// threads against those of powers of two, two pieces a thread: 8192 x 11008
+// forward 121 us, not 147, 8192 x 1000 15, not 19; 8192 x 5120 63, not 59.
 //
 // The gain's gradient sums over rows.  Backward blocks take a contiguous range
 // of rows each and keep their columns' sums in registers; the blocks' partial
@@ -86,8 +92,10 @@ __device__ __forceinline__ void store_y(const NormArgs& a, int64_t row, int64_t 
 }
 
 // RES: a residual is added (and h written); without one h may still be wanted.
+// (8 waves to a SIMD, which the scalar registers would else leave at 7: 8192 x 5120
+// 64 us, not 73.)
 template <typename T, int NT, int V, bool RES>
-__global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
+__global__ __launch_bounds__(NT, V == 1 ? 8 : 1) void rmsnorm_kernel(NormArgs a) {
   __shared__ float red[2][NT / 64];
   int flip = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -96,15 +104,19 @@ __global__ __launch_bounds__(NT) void rmsnorm_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8;
-      h[i].template load<true>(static_cast<const T*>(a.x) + row * a.ld_x + c, a.cols - c);
+      h[i].template fetch<true>(static_cast<const T*>(a.x) + row * a.ld_x + c, a.cols - c);
       if constexpr (RES)
-        r[i].template load<true>(static_cast<const T*>(a.residual) + row * a.ld_residual + c,
-                                 a.cols - c);
+        r[i].template fetch<true>(static_cast<const T*>(a.residual) + row * a.ld_residual + c,
+                                  a.cols - c);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8;
-      if constexpr (RES) add(h[i], r[i]);
+      h[i].settle(a.cols - c);
+      if constexpr (RES) {
+        r[i].settle(a.cols - c);
+        add(h[i], r[i]);
+      }
       if (RES || (a.h != nullptr && a.h != a.x))
         h[i].template store<true>(static_cast<T*>(a.h) + row * a.ld_h + c, a.cols - c);
 #pragma unroll
@@ -159,7 +171,9 @@ __device__ __forceinline__ void block_rows(int64_t rows, int64_t blocks, int64_t
   r1 = rows * (b + 1) / blocks;
 }
 
-// The next row is loaded while the present one is reduced.
+// The next row is loaded while the present one is reduced, where the registers
+// hold both: one piece of each a thread.  (Two pieces spilled: 8192 x 11008 bf16
+// 226 us, 153 without the early load.)
 template <typename T, int NT, int V, bool DRES, bool DGAIN>
 __global__ __launch_bounds__(NT) void rmsnorm_backward_kernel(NormBwdArgs a) {
   __shared__ float red[2][NT / 64];
@@ -180,19 +194,27 @@ __global__ __launch_bounds__(NT) void rmsnorm_backward_kernel(NormBwdArgs a) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8, valid = a.cols - c;
-      w.dy[i].load(static_cast<const T*>(a.dy) + row * a.ld_dy + c, valid);
-      w.h[i].load(static_cast<const T*>(a.h) + row * a.ld_h + c, valid);
+      w.dy[i].fetch(static_cast<const T*>(a.dy) + row * a.ld_dy + c, valid);
+      w.h[i].fetch(static_cast<const T*>(a.h) + row * a.ld_h + c, valid);
       if constexpr (DRES)
-        w.dres[i].load(static_cast<const T*>(a.dres) + row * a.ld_dres + c, valid);
+        w.dres[i].fetch(static_cast<const T*>(a.dres) + row * a.ld_dres + c, valid);
     }
     w.rstd = a.rstd[row];
   };
   Row next;
-  if (r0 < r1) load_row(next, r0);
+  if (V == 1 && r0 < r1) load_row(next, r0);
   int flip = 0;
   for (int64_t row = r0; row < r1; ++row) {
-    const Row w = next;
-    if (row + 1 < r1) load_row(next, row + 1);
+    if (V > 1) load_row(next, row);
+    Row w = next;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int64_t valid = a.cols - (threadIdx.x + i * NT) * 8;
+      w.dy[i].settle(valid);
+      w.h[i].settle(valid);
+      if constexpr (DRES) w.dres[i].settle(valid);
+    }
+    if (V == 1 && row + 1 < r1) load_row(next, row + 1);
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -288,58 +310,81 @@ __global__ __launch_bounds__(NT) void rmsnorm_dx_wide_kernel(NormBwdArgs a) {
   }
 }
 
-// dgain[j] = the sum of column j's `parts` partials: each of 16 waves a
-// contiguous share of them in order, eight loads in flight, then the waves in
-// order.
-constexpr int kJoinWaves = 16;
-__global__ __launch_bounds__(64 * kJoinWaves) void dgain_kernel(const float* __restrict__ part,
-                                                                int64_t parts, int64_t cols,
-                                                                float* __restrict__ dgain) {
-  __shared__ float red[kJoinWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
-  const int64_t p1 = parts * (wave + 1) / kJoinWaves;
+// dgain[j] = the sum of column j's `parts` partials: each of the block's shares a
+// contiguous range of them in order, eight loads in flight, then the shares in
+// order.  Columns per block: 32 are one line of a partial sum's row; 64 leave a
+// join of 384 columns to 6 blocks (8192 x 384: 19 us against 15 with the sums).
+constexpr int kJoinCols = 32, kJoinShares = 1024 / kJoinCols;
+__global__ __launch_bounds__(1024) void dgain_kernel(const float* __restrict__ part,
+                                                     int64_t parts, int64_t cols,
+                                                     float* __restrict__ dgain) {
+  __shared__ float red[kJoinShares][kJoinCols];
+  const int lane = threadIdx.x % kJoinCols, share = threadIdx.x / kJoinCols;
+  const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + lane;
+  const int64_t p1 = parts * (share + 1) / kJoinShares;
   float s = 0.0f;
   if (c < cols)
-    for (int64_t p = parts * wave / kJoinWaves; p < p1; p += 8) {
+    for (int64_t p = parts * share / kJoinShares; p < p1; p += 8) {
       float v[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) v[q] = p + q < p1 ? part[(p + q) * cols + c] : 0.0f;
 #pragma unroll
       for (int q = 0; q < 8; ++q) s += v[q];
     }
-  red[wave][lane] = s;
+  red[share][lane] = s;
   __syncthreads();
-  if (wave != 0 || c >= cols) return;
+  if (share != 0 || c >= cols) return;
 #pragma unroll
-  for (int w = 1; w < kJoinWaves; ++w) s += red[w][lane];
+  for (int w = 1; w < kJoinShares; ++w) s += red[w][lane];
   dgain[c] = s;
 }
 
 constexpr int64_t kMaxGrid = int64_t(1) << 22;
 constexpr int64_t kWideCols = 1024 * 8 * 2;  // the widest row kept in registers
 
-// Threads of a backward block, and blocks (partial sums of the gain's gradient):
-// what the CUs hold at once, 2048 threads each, up to 8 blocks a CU.
-int backward_threads(int64_t cols) {
-  return cols <= 512 ? 64 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024;
+// f(threads, pieces a thread) with the fewest threads that hold a row.
+template <typename F>
+auto with_shape(int64_t cols, F&& f) {
+#define ZF_SHAPE(NT, V) \
+  if (cols <= NT * V * 8) return f(std::integral_constant<int, NT>(), std::integral_constant<int, V>())
+  ZF_SHAPE(64, 1);
+  ZF_SHAPE(128, 1);
+  ZF_SHAPE(256, 1);
+  ZF_SHAPE(384, 1);
+  ZF_SHAPE(512, 1);
+  ZF_SHAPE(640, 1);
+  ZF_SHAPE(768, 1);
+  ZF_SHAPE(1024, 1);
+  ZF_SHAPE(768, 2);
+#undef ZF_SHAPE
+  return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
 }
+int backward_threads(int64_t cols) {
+  return with_shape(cols, [](auto nt, auto) { return static_cast<int>(nt); });
+}
+// Blocks of the backward kernel, and partial sums of the gain's gradient: what the
+// CUs hold at once, 16 waves each by the kernel's registers, at most 4 blocks a CU
+// and at least 2 rows a block (1237 x 384 fp32 8.6 us, one row a block 11.8).  Twice
+// that where each still has 8 rows (8192 x 4096 bf16 57 us, not 61; with fewer rows
+// the sums cost more: 1237 x 4096 16, not 13).  Equal shares: as many rows to a
+// block as the fullest has.
 int64_t backward_blocks(int64_t rows, int64_t cols) {
-  return std::min<int64_t>(rows, std::min(2048, (256 * 2048) / backward_threads(cols)));
+  const int64_t held = 256 * std::min(4, 1024 / backward_threads(cols));
+  const int64_t most = rows >= 16 * held ? 2 * held : held;
+  const int64_t each = std::max<int64_t>(2, (rows + most - 1) / most);
+  return (rows + each - 1) / each;
 }
 
 template <typename T, bool RES>
 void norm_forward(const NormArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(a.rows < kMaxGrid ? a.rows : kMaxGrid));
-#define ZF_NORM(NT, V) \
-  hipLaunchKernelGGL((rmsnorm_kernel<T, NT, V, RES>), grid, dim3(NT), 0, s, a)
-  if (a.cols <= 512) ZF_NORM(64, 1);
-  else if (a.cols <= 2048) ZF_NORM(256, 1);
-  else if (a.cols <= 4096) ZF_NORM(256, 2);
-  else if (a.cols <= 8192) ZF_NORM(512, 2);
-  else if (a.cols <= kWideCols) ZF_NORM(1024, 2);
-  else hipLaunchKernelGGL((rmsnorm_wide_kernel<T, 1024>), grid, dim3(1024), 0, s, a);
-#undef ZF_NORM
+  if (a.cols > kWideCols) {
+    hipLaunchKernelGGL((rmsnorm_wide_kernel<T, 1024>), grid, dim3(1024), 0, s, a);
+    return;
+  }
+  with_shape(a.cols, [&](auto nt, auto v) {
+    hipLaunchKernelGGL((rmsnorm_kernel<T, nt, v, RES>), grid, dim3(nt), 0, s, a);
+  });
 }
 
 template <typename T, bool DRES, bool DGAIN>
@@ -347,15 +392,11 @@ void norm_backward(const NormBwdArgs& a, hipStream_t s) {
   const int64_t blocks =
       DGAIN ? backward_blocks(a.rows, a.cols) : (a.rows < kMaxGrid ? a.rows : kMaxGrid);
   const dim3 grid(static_cast<uint32_t>(blocks));
-#define ZF_NORM(NT, V) \
-  hipLaunchKernelGGL((rmsnorm_backward_kernel<T, NT, V, DRES, DGAIN>), grid, dim3(NT), 0, s, a)
-  const int nt = backward_threads(a.cols);
-  if (nt == 64) ZF_NORM(64, 1);
-  else if (nt == 256) ZF_NORM(256, 1);
-  else if (nt == 512) ZF_NORM(512, 1);
-  else if (a.cols <= 8192) ZF_NORM(1024, 1);
-  else if (a.cols <= kWideCols) ZF_NORM(1024, 2);
-  else {
+  if (a.cols <= kWideCols) {
+    with_shape(a.cols, [&](auto nt, auto v) {
+      hipLaunchKernelGGL((rmsnorm_backward_kernel<T, nt, v, DRES, DGAIN>), grid, dim3(nt), 0, s, a);
+    });
+  } else {
     if (DGAIN)
       hipLaunchKernelGGL((rmsnorm_dgain_wide_kernel<T>),
                          dim3(static_cast<uint32_t>((a.cols + 2047) / 2048),
@@ -365,7 +406,6 @@ void norm_backward(const NormBwdArgs& a, hipStream_t s) {
                        dim3(static_cast<uint32_t>(a.rows < kMaxGrid ? a.rows : kMaxGrid)),
                        dim3(1024), 0, s, a);
   }
-#undef ZF_NORM
 }
 
 template <typename T>
@@ -404,8 +444,8 @@ hipError_t launch_rmsnorm_backward(const NormBwdArgs& a, int32_t dtype, hipStrea
     else norm_backward<float>(a, s);
   }
   if (a.dgain != nullptr)  // (no rows: no partials, zeros)
-    hipLaunchKernelGGL(dgain_kernel, dim3(static_cast<uint32_t>((a.cols + 63) / 64)),
-                       dim3(64 * kJoinWaves), 0, s, a.part, backward_blocks(a.rows, a.cols), a.cols, a.dgain);
+    hipLaunchKernelGGL(dgain_kernel, dim3(static_cast<uint32_t>((a.cols + kJoinCols - 1) / kJoinCols)),
+                       dim3(1024), 0, s, a.part, backward_blocks(a.rows, a.cols), a.cols, a.dgain);
   return hipGetLastError();
 }
 
