@@ -149,6 +149,22 @@ __device__ __forceinline__ void wait_reads() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// The first `valid` of a 16-byte unit's elements.
+__device__ __forceinline__ void store_units(uint16_t* out, u32x4 v, int64_t valid) {
+  Vec8<uint16_t> u;
+  u.u = v;
+  u.store(out, valid);
+}
+__device__ __forceinline__ void store_units(float* out, u32x4 v, int64_t valid) {
+  uint32_t* const q = reinterpret_cast<uint32_t*>(out);
+  if (valid >= 4) {
+    *reinterpret_cast<u32x4_f*>(q) = v;
+  } else if (valid > 0) {
+    if (valid & 2) *reinterpret_cast<u32x2_f*>(q) = u32x2{v.x, v.y};
+    if (valid & 1) q[valid - 1] = valid & 2 ? v.z : v.x;
+  }
+}
+
 // A 256-thread block computes a BM x BN tile, each wave a quarter of it, from two
 // slots of 128 elements of the reduction in LDS.  Each half of a step multiplies
 // 64 elements from registers while the next 64 are read from LDS.  Memory is
@@ -371,9 +387,8 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
     } else {
 #pragma unroll 1
       for (int r = lane / kRun; r < 32 && 32 * i + r < rows; r += kStep)
-#pragma unroll 1
-        for (int q = 0; q < kPer && c + q < cols; ++q)
-          out[(32 * i + r) * p.ld_out + c + q] = slab[r * kPitch + c + q];
+        store_units(out + (32 * i + r) * p.ld_out + c,
+                    *reinterpret_cast<const u32x4*>(slab + r * kPitch + c), cols - c);
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -549,7 +564,8 @@ void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
   // 352 / 402, 1024 x 11008 x 4096 (172 / 344 / 688 tiles) 49 / 58 / 52, 2048 x
   // 4096 x 11008 (128 / 256 / 512) 118 / 92 / 104, 1024 x 4096 x 4096 (64 / 128 /
   // 256) 44 / 29 / 24.  The precise form is bound by its products: 128 x 256 and
-  // 128 x 128 within 2% from 2048 x 4096 x 4096 on, 48 / 45 at 1003 x 5003 x 3001.
+  // 128 x 128 within 2% from 2048 x 4096 x 4096 on, 48 / 45 at 1003 x 5003 x 3001;
+  // 128 x 192 46 there and 296, not 236, at 8192 x 4096 x 4096.
   if constexpr (!PRECISE) {
     if (tiles(a.m, a.n, 256, 256) >= 160) {
       ZF_TILES(256, 256, false, 1, a);
