@@ -279,3 +279,13 @@ def test_linear_layer_gradients():
     product_check(dq, wt, v64(dy, 1), v64(w.t(), 128), torch.bfloat16)
     product_check(dt, xt, v64(dy.t(), 1), v64(x.t(), 1), torch.bfloat16)
     product_check(xt, dt, v64(x.t(), 1), v64(dy.t(), 1), torch.float32)
+
+
+@pytest.mark.parametrize("n", range(257, 265))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_every_tail(n, dtype):
+    """Rows that end at each element of a 16-byte unit: of the product's result, and
+    of what is quantised."""
+    test_matmul(40, n, 130, (1, 1), dtype)
+    test_quantize((40, n), dtype, 1, 1, 0)
+    test_quantize((40, n), dtype, 128, 0, 1)

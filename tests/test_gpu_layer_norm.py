@@ -182,3 +182,18 @@ def test_no_rows():
     assert out.y.shape == (0, 5)
     dx, dgain = zf.rmsnorm_backward(x, x, g, out.rstd, dgain=torch.full((5,), 3.0, device="cuda"))
     assert dx.shape == (0, 5) and (dgain == 0).all()
+
+
+@pytest.mark.parametrize("cols", [*range(65, 73), 512, 1025, 2047, 2049, 3080, 4102, 5123, 6145,
+                                  8193, 11007, 12289, 16383])
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f32"])
+def test_every_tail_and_block(cols, dtype):
+    """Rows that end at each element of a thread's eight, and rows either side of
+    each number of threads."""
+    test_forward((3, cols), dtype, True, 1)
+    test_backward((3, cols), dtype, True, 1)
+
+
+@pytest.mark.parametrize("shape", [(16500, 40), (4111, 4100)], ids=str)
+def test_backward_many_rows(shape):
+    test_backward(shape, torch.bfloat16, True, 0)
