@@ -9,7 +9,9 @@
 // transposed copy's 8 x 8 byte blocks pass through LDS so that both copies are
 // written in lines of 128 bytes.  Bound by HBM: 2 bytes read and 1 written per
 // element and copy (bf16, both copies: 8192 x 11008 68 us, 5.3 TB/s; 4096 x 11008
-// 37 us, 4.9; 4099 x 5003, whose rows begin anywhere in a line, 17.4 us, 4.7).
+// 37 us, 4.9; 4099 x 5003, whose rows begin anywhere in a line, 16 us with one scale
+// a block).  Four blocks a CU: with six (lane offsets in 32 bits) 4096 x 11008 takes
+// 38.7 us, not 37.6.
 #include "zf_layer.hpp"
 
 namespace zf {
@@ -122,8 +124,10 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
   B x;
 #pragma unroll
   for (int p = 0; p < 8; ++p)
-    x.v[p].template load<NT>(static_cast<const T*>(a.x) + (r0 + p) * a.ld_x + c0,
-                            r0 + p < a.rows ? a.cols - c0 : 0);
+    x.v[p].template fetch<NT>(static_cast<const T*>(a.x) + (r0 + p) * a.ld_x + c0,
+                             r0 + p < a.rows ? a.cols - c0 : 0);
+#pragma unroll
+  for (int p = 0; p < 8; ++p) x.v[p].settle(r0 + p < a.rows ? a.cols - c0 : 8);
 
   uint32_t rm[8], cm[B::kMax];
   x.maxima(rm, cm);
