@@ -512,7 +512,11 @@ __global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p) {
 
 // ---- choice of a form --------------------------------------------------------
 
-constexpr int64_t kRowsMax = 16;  // rows of a up to which matmul_rows_kernel is taken
+// Rows of a up to which matmul_rows_kernel is taken, and rows of b that its blocks
+// of 16 still reach in one dispatch (of fewer than 2^32 threads).
+constexpr int64_t kRowsMax = 16;
+constexpr int64_t kRowsReach = int64_t(1) << 27;
+bool takes_rows(int64_t m, int64_t n) { return m <= kRowsMax && n <= kRowsReach; }
 
 int64_t tiles(const int64_t m, const int64_t n, int bm, int bn) {
   return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
@@ -524,7 +528,7 @@ int64_t tiles(const int64_t m, const int64_t n, int bm, int bn) {
 // result is written and read at some 6 TB/s, the joining launch costs 3.  E.g.
 // 512 x 1024 x 11008: 1 share 41 us, 8 shares 20.6; 256 x 4096 x 4096 18.1, 17.1.
 int shares(int64_t m, int64_t n, int64_t k, bool precise) {
-  if (m <= kRowsMax) return 1;
+  if (takes_rows(m, n)) return 1;
   const int64_t t = tiles(m, n, 128, 128), steps = (k + kBK - 1) / kBK;
   if (t > 160) return 1;
   int best = 1;
@@ -608,7 +612,7 @@ size_t matmul_workspace(int64_t m, int64_t n, int64_t k) {
 
 hipError_t launch_matmul(const MatmulArgs& a, void* ws, hipStream_t s) {
   (void)hipGetLastError();
-  if (a.m <= kRowsMax) {
+  if (takes_rows(a.m, a.n)) {
     if (a.out_f32) launch_rows<true>(a, s);
     else launch_rows<false>(a, s);
   } else {

@@ -320,26 +320,31 @@ __global__ __launch_bounds__(1024) void dgain_kernel(const float* __restrict__ p
                                                      float* __restrict__ dgain) {
   __shared__ float red[kJoinShares][kJoinCols];
   const int lane = threadIdx.x % kJoinCols, share = threadIdx.x / kJoinCols;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * kJoinCols + lane;
   const int64_t p1 = parts * (share + 1) / kJoinShares;
-  float s = 0.0f;
-  if (c < cols)
-    for (int64_t p = parts * share / kJoinShares; p < p1; p += 8) {
-      float v[8];
+  for (int64_t c0 = static_cast<int64_t>(blockIdx.x) * kJoinCols; c0 < cols;
+       c0 += static_cast<int64_t>(gridDim.x) * kJoinCols) {
+    const int64_t c = c0 + lane;
+    float s = 0.0f;
+    if (c < cols)
+      for (int64_t p = parts * share / kJoinShares; p < p1; p += 8) {
+        float v[8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = p + q < p1 ? part[(p + q) * cols + c] : 0.0f;
+        for (int q = 0; q < 8; ++q) v[q] = p + q < p1 ? part[(p + q) * cols + c] : 0.0f;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) s += v[q];
+        for (int q = 0; q < 8; ++q) s += v[q];
+      }
+    red[share][lane] = s;
+    __syncthreads();
+    if (share == 0 && c < cols) {
+#pragma unroll
+      for (int w = 1; w < kJoinShares; ++w) s += red[w][lane];
+      dgain[c] = s;
     }
-  red[share][lane] = s;
-  __syncthreads();
-  if (share != 0 || c >= cols) return;
-#pragma unroll
-  for (int w = 1; w < kJoinShares; ++w) s += red[w][lane];
-  dgain[c] = s;
+    __syncthreads();
+  }
 }
 
-constexpr int64_t kMaxGrid = int64_t(1) << 22;
+constexpr int64_t kMaxGrid = int64_t(1) << 21;  // blocks; a dispatch holds fewer than 2^32 threads
 constexpr int64_t kWideCols = 1024 * 8 * 2;  // the widest row kept in registers
 
 // f(threads, pieces a thread) with the fewest threads that hold a row.
@@ -444,8 +449,10 @@ hipError_t launch_rmsnorm_backward(const NormBwdArgs& a, int32_t dtype, hipStrea
     else norm_backward<float>(a, s);
   }
   if (a.dgain != nullptr)  // (no rows: no partials, zeros)
-    hipLaunchKernelGGL(dgain_kernel, dim3(static_cast<uint32_t>((a.cols + kJoinCols - 1) / kJoinCols)),
-                       dim3(1024), 0, s, a.part, backward_blocks(a.rows, a.cols), a.cols, a.dgain);
+    hipLaunchKernelGGL(
+        dgain_kernel,
+        dim3(static_cast<uint32_t>(std::min<int64_t>((a.cols + kJoinCols - 1) / kJoinCols, kMaxGrid))),
+        dim3(1024), 0, s, a.part, backward_blocks(a.rows, a.cols), a.cols, a.dgain);
   return hipGetLastError();
 }
 

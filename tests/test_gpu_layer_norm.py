@@ -197,3 +197,9 @@ def test_every_tail_and_block(cols, dtype):
 @pytest.mark.parametrize("shape", [(16500, 40), (4111, 4100)], ids=str)
 def test_backward_many_rows(shape):
     test_backward(shape, torch.bfloat16, True, 0)
+
+
+def test_more_rows_than_blocks():
+    """A dispatch has at most 2^21 blocks; its rows are walked in strides."""
+    test_forward((2 ** 21 + 5, 8), torch.bfloat16, True, 0)
+    test_backward((2 ** 21 + 5, 8), torch.bfloat16, True, 0)
