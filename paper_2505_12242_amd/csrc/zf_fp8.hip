@@ -26,13 +26,6 @@ __device__ __forceinline__ int t_off(int c, int u) {
   return c * kTile + ((((u >> 1) ^ (c >> 3)) & 7) << 4) + ((u & 1) << 3);
 }
 
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
-                                                                __builtin_bit_cast(u16x2, b)));
-}
-
 // A thread's 8 x 8 elements.  bf16 ones stay packed in pairs, two columns a word,
 // and their magnitudes are compared as 16-bit integers, two at a time.
 template <typename T>

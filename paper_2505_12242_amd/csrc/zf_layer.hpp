@@ -253,6 +253,13 @@ __device__ __forceinline__ uint32_t max16(uint32_t x) {
   x = max(x, dpp<0x122>(x));
   return max(x, dpp<0x121>(x));
 }
+// The larger 16-bit integers of each pair.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                __builtin_bit_cast(u16x2, b)));
+}
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 // The e8m0 code of a group whose largest magnitude has these bits: the least

@@ -2,19 +2,16 @@
 // the reduction (formulas and format in zf_layer.h).
 //
 // out[i][j] = sum over groups g of 2^(ca[i][g] + cb[j][g] - 254) * sum over
-// the group of a * b.  The scaled matrix instruction of gfx950 takes the codes
-// beside the operands, so nothing is rescaled between groups.
+// the group of a * b, products and sums in fp32 (to_bf16 below says on which
+// instruction, and why).
 //
-// Three forms.  Many rows: tiles of 256 x 256, 128 x 256 or 128 x 128
-// (matmul_tile_kernel), bound by what the chip's power lets the matrix units do
-// and by L2: 2.37-2.65 PFLOP/s at 8192 x 11008 x 4096, 8192 x 4096 x 11008 and
-// 4096 x 11008 x 8192, where the same kernel without its loads reaches 3.1 and
-// the instruction alone on constant data 4.6.  Few tiles: the reduction is split
-// over blocks and the shares' results joined in order (64 x 11008 x 4096: 17 us).
-// Up to 16 rows: the second operand's bytes are all that counts
-// (matmul_rows_kernel; 1 x 11008 x 4096: 45 MB in 9.9 us, 4.6 TB/s).
+// Three forms.  Many rows: tiles of 128 x 128 (matmul_tile_kernel), bound by the
+// bf16 instruction's rate and the conversions before it: 1.12-1.16 PFLOP/s at 8192 x
+// 11008 x 4096, 8192 x 4096 x 11008, 4096 x 11008 x 8192 and 2048 x 4096 x 11008.  Few
+// tiles: the reduction is split over blocks and the shares' results joined in order
+// (64 x 11008 x 4096: 22 + 4 us).  Up to 16 rows: the second operand's bytes are all
+// that counts (matmul_rows_kernel; 1 x 11008 x 4096: 45 MB in 11.5 us, 4.0 TB/s).
 #include <algorithm>
-#include <type_traits>
 
 #include "zf_layer.hpp"
 
@@ -24,11 +21,16 @@ namespace {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 typedef __bf16 v4b __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int kBK = 128;  // reduction per step: one scale group
+// A block's tile, a wave's quarter of it, that in 32 x 32 tiles, and fragments of
+// half a step (64 rows of the block's tile each).
+constexpr int kBM = 128, kBN = 128, kWM = kBM / 2, kWN = kBN / 2, kTM = kWM / 32, kTN = kWN / 32;
+constexpr int kParts = kTM + kTN;
 
 // A step's rows in LDS: 16-byte unit c (of 8) of row r lies at this byte.  16
 // consecutive rows reading one unit meet all 64 banks once.
@@ -36,17 +38,12 @@ __device__ __forceinline__ int tile_off(int r, int c) {
   return r * kBK + ((c ^ ((r >> 1) & 7)) << 4);
 }
 
-// One phase of a wave: acc[i][j] += y_j x_i^T (32 x 32 tiles) over 64 elements of
-// the reduction, of which a lane holds 32 of row lane % 32 of each tile.  y's
-// rows run along the accumulator's registers, x's along its lanes.  Two forms:
-//   fast     the scaled 8-bit instruction.  It aligns 64 products to the
-//            largest of them and cuts what lies some 2^-13 below (measured:
-//            1.3e-5 relative on normal data), far less than the 2^-4 that e4m3
-//            itself cut and the 2^-9 of a bf16 result.
-//   precise  elements times scale to bf16 (exact), products and sums in fp32
-//            (7e-9 relative), at 0.42 of the rate.  Taken for fp32 results.
-__device__ __forceinline__ void to_bf16(v8i x, int code, v8b (&out)[4]) {
-  const float s = __uint_as_float(static_cast<uint32_t>(code & 255) << 23);
+// The 8-bit matrix instruction aligns every 8 products to the largest of them and
+// cuts what lies 2^-15 below it (1.3e-5 relative on normal data, any share of a
+// result that cancels).  So elements times scale go to bf16, which holds them
+// exactly, and products and sums are the bf16 instruction's, in fp32 (7e-9), at
+// 0.42 of the 8-bit rate.  s: the scale; an infinity's bits stand for a NaN's code.
+__device__ __forceinline__ void to_bf16(v8i x, float s, v8b (&out)[4]) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * q], s, false);
@@ -56,31 +53,29 @@ __device__ __forceinline__ void to_bf16(v8i x, int code, v8b (&out)[4]) {
     out[q] = v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   }
 }
-// Tiles [G TM TN / (TM + TN), (G + 1) TM TN / (TM + TN)) of a phase (row by row of
-// acc); cvt holds the precise form's y, and its x of the row at hand.
-template <int TM, int TN>
+
+// One phase of a wave: acc[i][j] += y_j x_i^T (32 x 32 tiles) over 64 elements of
+// the reduction, of which a lane holds 32 of row lane % 32 of each tile.  y's
+// rows run along the accumulator's registers, x's along its lanes.  Tiles
+// [G TM TN / (TM + TN), (G + 1) TM TN / (TM + TN)) of it (row by row of acc); cvt
+// holds the phase's y in bf16, and its x of the row at hand.
 struct Converted {
-  v8b x[4], y[TN][4];
+  v8b x[4], y[kTN][4];
 };
-template <bool PRECISE, int G, int TM, int TN>
-__device__ __forceinline__ void mma(const v8i (&x)[TM], const int (&cx)[TM], const v8i (&y)[TN],
-                                    const int (&cy)[TN], v16f (&acc)[TM][TN],
-                                    Converted<TM, TN>& cvt) {
-  if constexpr (PRECISE && G == 0)
+template <int G>
+__device__ __forceinline__ void mma(const v8i (&x)[kTM], const float (&sx)[kTM],
+                                    const v8i (&y)[kTN], const float (&sy)[kTN],
+                                    v16f (&acc)[kTM][kTN], Converted& cvt) {
+  if constexpr (G == 0)
 #pragma unroll
-    for (int j = 0; j < TN; ++j) to_bf16(y[j], cy[j], cvt.y[j]);
+    for (int j = 0; j < kTN; ++j) to_bf16(y[j], sy[j], cvt.y[j]);
 #pragma unroll
-  for (int t = G * TM * TN / (TM + TN); t < (G + 1) * TM * TN / (TM + TN); ++t) {
-    const int i = t / TN, j = t % TN;
-    if constexpr (!PRECISE) {
-      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(y[j], x[i], acc[i][j], 0, 0, 0,
-                                                                  cy[j], 0, cx[i]);
-    } else {
-      if (j == 0) to_bf16(x[i], cx[i], cvt.x);
+  for (int t = G * kTM * kTN / kParts; t < (G + 1) * kTM * kTN / kParts; ++t) {
+    const int i = t / kTN, j = t % kTN;
+    if (j == 0) to_bf16(x[i], sx[i], cvt.x);
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cvt.y[j][q], cvt.x[q], acc[i][j], 0, 0, 0);
-    }
+    for (int q = 0; q < 4; ++q)
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cvt.y[j][q], cvt.x[q], acc[i][j], 0, 0, 0);
 #ifdef __HIP_DEVICE_COMPILE__  // (the host's pass does not know the registers)
     // (keeps the product from being moved behind what follows)
     asm volatile("" : "+a"(acc[i][j]));
@@ -165,7 +160,7 @@ __device__ __forceinline__ void store_units(float* out, u32x4 v, int64_t valid) 
   }
 }
 
-// A 256-thread block computes a BM x BN tile, each wave a quarter of it, from two
+// A 256-thread block computes a 128 x 128 tile, each wave a quarter of it, from two
 // slots of 128 elements of the reduction in LDS.  Each half of a step multiplies
 // 64 elements from registers while the next 64 are read from LDS.  Memory is
 // loaded straight to LDS, in whole 128-byte lines, spread evenly over the
@@ -173,26 +168,29 @@ __device__ __forceinline__ void store_units(float* out, u32x4 v, int64_t valid) 
 // memory pipeline holds up the products behind it.  Rows past an operand's end
 // repeat its last row (their results are not stored); the units past the
 // reduction's end repeat the row's last one and are cleared in LDS.
-template <int BM, int BN, bool PRECISE, bool PART>
+// Scales are taken relative to the largest of their row (of this share of the
+// reduction), and the results multiplied by both rows' largest at the end: what
+// bf16 and the sums can hold does not depend on where the scales lie.  PART: the
+// results are a share's, in fp32.
+template <typename Out, bool PART>
 __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
-  constexpr int WM = BM / 2, WN = BN / 2, TM = WM / 32, TN = WN / 32;
-  constexpr int kRows = BM + BN;
+  constexpr int kRows = kBM + kBN;
   constexpr int kSlot = kRows * kBK;
-  constexpr int kParts = TM + TN;  // fragments of half a step; 64 rows of the tile each
-  constexpr int kCodeUnits = (kRows + 255) / 256;  // of 64 rows' codes, per four steps
-  constexpr int kLoads = 2 * kParts + 1;  // of a wave per step: 8 rows each, and a part of the codes
+  constexpr int kLoads = 2 * kParts + 1;  // of a wave per step: 8 rows each, and 64 rows' codes
   constexpr int kCodes = 2 * kSlot;       // a word (four steps) a row, two groups of steps
+  constexpr int kTops = kCodes + 2 * kRows * 4;  // a row's exponent of its largest scale
   // A step's 2 kParts groups of products.  Groups kOpen .. issue its loads.
-  constexpr int kOpen = TM / 2, kOpenB = kParts / 2, kIssue = 2 * kParts - kOpen;
-  static_assert(TM % 2 == 0 && TN % 2 == 0, "two fragments are read at a time");
-  static_assert((kOpenB - kOpen) * kLoads / kIssue <= 2 * TM, "rows of x alone until y's are read");
-  __shared__ __align__(1024) uint8_t lds[kCodes + 2 * kRows * 4];
+  constexpr int kOpen = kTM / 2, kOpenB = kParts / 2, kIssue = 2 * kParts - kOpen;
+  static_assert(kTM % 2 == 0 && kTN % 2 == 0, "two fragments are read at a time");
+  static_assert(kRows == 256, "a row of either operand a thread");
+  static_assert((kOpenB - kOpen) * kLoads / kIssue <= 2 * kTM, "rows of x alone until y's are read");
+  __shared__ __align__(1024) uint8_t lds[kTops + kRows * 4];
   const int t = threadIdx.x, lane = t & 63, wave = uniform_i32(t >> 6);
-  const int wm = (wave & 1) * WM, wn = (wave >> 1) * WN;
+  const int wm = (wave & 1) * kWM, wn = (wave >> 1) * kWN;
   uint32_t mi, ni;
-  tile_of(blockIdx.x, static_cast<uint32_t>((p.m + BM - 1) / BM),
-          static_cast<uint32_t>((p.n + BN - 1) / BN), mi, ni);
-  const int64_t m0 = static_cast<int64_t>(mi) * BM, n0 = static_cast<int64_t>(ni) * BN;
+  tile_of(blockIdx.x, static_cast<uint32_t>((p.m + kBM - 1) / kBM),
+          static_cast<uint32_t>((p.n + kBN - 1) / kBN), mi, ni);
+  const int64_t m0 = static_cast<int64_t>(mi) * kBM, n0 = static_cast<int64_t>(ni) * kBN;
   // this share's steps [first, steps), the first a multiple of four
   const int all = static_cast<int>((p.k + kBK - 1) / kBK);
   const int first = PART ? static_cast<int>(blockIdx.y) * p.share : 0;
@@ -203,24 +201,20 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   const rsrc_t ra = make_rsrc(p.a.data + m0 * p.a.ld, -1), rb = make_rsrc(p.b.data + n0 * p.b.ld, -1);
   const rsrc_t rca = make_rsrc(p.a.scale + (m0 >> p.a.shift) * p.a.ld_scale, -1);
   const rsrc_t rcb = make_rsrc(p.b.scale + (n0 >> p.b.shift) * p.b.ld_scale, -1);
-  const int last_a = static_cast<int>(min<int64_t>(BM, p.m - m0)) - 1;
-  const int last_b = static_cast<int>(min<int64_t>(BN, p.n - n0)) - 1;
+  const int last_a = static_cast<int>(min<int64_t>(kBM, p.m - m0)) - 1;
+  const int last_b = static_cast<int>(min<int64_t>(kBN, p.n - n0)) - 1;
   // Load i < 2 kParts covers 8 rows of every wave: together 32 of part i / 2's 64.
-  uint32_t row[2 * kParts], code_row[kCodeUnits];
+  uint32_t row[2 * kParts];
 #pragma unroll
   for (int i = 0; i < 2 * kParts; ++i) {
     const int r = 8 * (wave + 4 * i) + (lane >> 3);
-    row[i] = 32 * i < BM ? static_cast<uint32_t>(min(r, last_a)) * static_cast<uint32_t>(p.a.ld)
-                         : static_cast<uint32_t>(min(r - BM, last_b)) * static_cast<uint32_t>(p.b.ld);
+    row[i] = 32 * i < kBM ? static_cast<uint32_t>(min(r, last_a)) * static_cast<uint32_t>(p.a.ld)
+                         : static_cast<uint32_t>(min(r - kBM, last_b)) * static_cast<uint32_t>(p.b.ld);
   }
-  const auto code_unit = [&](int i) { return min(wave + 4 * i, kRows / 64 - 1); };
-#pragma unroll
-  for (int i = 0; i < kCodeUnits; ++i) {
-    const int r = 64 * code_unit(i) + lane;
-    code_row[i] = 64 * code_unit(i) < BM
-        ? static_cast<uint32_t>(min(r, last_a) >> p.a.shift) * static_cast<uint32_t>(p.a.ld_scale)
-        : static_cast<uint32_t>(min(r - BM, last_b) >> p.b.shift) * static_cast<uint32_t>(p.b.ld_scale);
-  }
+  const uint32_t code_row =
+      t < kBM ? static_cast<uint32_t>(min(t, last_a) >> p.a.shift) * static_cast<uint32_t>(p.a.ld_scale)
+              : static_cast<uint32_t>(min(t - kBM, last_b) >> p.b.shift) *
+                    static_cast<uint32_t>(p.b.ld_scale);
 
   // Step kt from memory to a slot, 16 bytes a lane: the lane's place in LDS is
   // fixed, so it loads the unit that tile_off puts there (past the reduction's
@@ -228,7 +222,7 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   const uint32_t unit = ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) << 4;
   const uint32_t last_unit = tail ? ((tail + 15) / 16 - 1) * 16 : 112;
   const auto load_rows = [&](int kt, int slot, int i) {
-    load_lds16(32 * i < BM ? ra : rb, lds + slot * kSlot + wave * 1024 + i * 4096,
+    load_lds16(32 * i < kBM ? ra : rb, lds + slot * kSlot + wave * 1024 + i * 4096,
                row[i] + min(unit, kt + 1 == steps ? last_unit : 112u), kt * kBK);
   };
   const auto load_step = [&](int kt, int slot) {
@@ -241,45 +235,51 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
     for (int r = t; r < kRows; r += 256)
       for (int c = tail / 16; c < 8; ++c) {
         u32x4* const u = reinterpret_cast<u32x4*>(
-            lds + slot * kSlot + (r < BM ? tile_off(r, c) : BM * kBK + tile_off(r - BM, c)));
+            lds + slot * kSlot + (r < kBM ? tile_off(r, c) : kBM * kBK + tile_off(r - kBM, c)));
         *u = clear_tail(*u, tail - 16 * c);
       }
     __syncthreads();
   };
-  // The codes of the four steps of group g, 64 rows of them.
-  const auto load_codes = [&](int g, int i) {
-    load_lds4(64 * code_unit(i) < BM ? rca : rcb,
-              lds + kCodes + (g & 1) * kRows * 4 + code_unit(i) * 256, code_row[i], 4 * g);
+  // The codes of the four steps of group g.
+  const auto load_codes = [&](int g) {
+    load_lds4(64 * wave < kBM ? rca : rcb, lds + kCodes + (g & 1) * kRows * 4 + wave * 256, code_row,
+              4 * g);
   };
 
-  v16f acc[TM][TN];
+  v16f acc[kTM][kTN];
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
+  for (int i = 0; i < kTM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < kTN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
-  v8i xa[2][TM], yb[2][TN];
-  int ca[TM], cb[TN];
-  Converted<TM, TN> cvt;
+  v8i xa[2][kTM], yb[2][kTN];
+  float sa[kTM], sb[kTN];
+  int top_a[kTM], top_b[kTN];
+  Converted cvt;
   const auto read_part = [&](int slot, int h, int i) {
     const uint8_t* const s = lds + slot * kSlot;
     const int c = 4 * h + 2 * (lane >> 5);
-    const int r = (i < TM ? wm + 32 * i : wn + 32 * (i - TM)) + (lane & 31);
-    const uint8_t* const q = s + (i < TM ? 0 : BM * kBK);
+    const int r = (i < kTM ? wm + 32 * i : wn + 32 * (i - kTM)) + (lane & 31);
+    const uint8_t* const q = s + (i < kTM ? 0 : kBM * kBK);
     const v8i v = join(*reinterpret_cast<const u32x4*>(q + tile_off(r, c)),
                        *reinterpret_cast<const u32x4*>(q + tile_off(r, c + 1)));
-    if (i < TM) xa[h][i < TM ? i : 0] = v;
-    else yb[h][i < TM ? 0 : i - TM] = v;
+    if (i < kTM) xa[h][i < kTM ? i : 0] = v;
+    else yb[h][i < kTM ? 0 : i - kTM] = v;
   };
-  const auto read_codes = [&](int kt, int(&ca)[TM], int(&cb)[TN]) {
+  int* const tops = reinterpret_cast<int*>(lds + kTops);
+  const auto read_scales = [&](int kt, float(&sa)[kTM], float(&sb)[kTN]) {
     const uint32_t* const w =
         reinterpret_cast<const uint32_t*>(lds + kCodes + ((kt >> 2) & 1) * kRows * 4) + (lane & 31);
+    const auto scale = [&](uint32_t word, int top) {
+      const int code = static_cast<int>(word >> (8 * (kt & 3)) & 255u) - top;
+      return __uint_as_float(static_cast<uint32_t>(max(code, 0)) << 23);
+    };
 #pragma unroll
-    for (int i = 0; i < TM; ++i) ca[i] = static_cast<int>(w[wm + 32 * i] >> (8 * (kt & 3)));
+    for (int i = 0; i < kTM; ++i) sa[i] = scale(w[wm + 32 * i], top_a[i]);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) cb[j] = static_cast<int>(w[BM + wn + 32 * j] >> (8 * (kt & 3)));
+    for (int j = 0; j < kTN; ++j) sb[j] = scale(w[kBM + wn + 32 * j], top_b[j]);
   };
 
   // Step kt, in 2 kParts groups of products, of its first half and then of its
@@ -290,17 +290,39 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   // at the half's start (behind them, y's and what kt + 2 has issued may still
   // be in flight), those of y where it reaches them.  Past the last step the
   // last one is loaded and read again, into a slot that nothing uses: the loop
-  // has no branch.  The codes of the next four steps are loaded one part a step.
+  // has no branch.  The codes of the next four steps are loaded with each step.
   const int last_group = (steps - 1) >> 2;
   if (first < steps) {
-#pragma unroll
-    for (int i = 0; i < kCodeUnits; ++i) load_codes(first >> 2, i);
+    load_codes(first >> 2);
     load_step(first, 0);
     load_step(min(first + 1, steps - 1), 1);
-    load_codes(min((first >> 2) + 1, last_group), 0);
+    load_codes(min((first >> 2) + 1, last_group));
+    // The thread's row's largest code less 127, 64 codes at a time (what follows
+    // the last step's may be anything).  With a NaN's among them, 0: it stays one.
+    const uint32_t* const codes = reinterpret_cast<const uint32_t*>(
+        t < kBM ? p.a.scale + (m0 >> p.a.shift) * p.a.ld_scale + code_row
+                : p.b.scale + (n0 >> p.b.shift) * p.b.ld_scale + code_row);
+    uint32_t most = 0;  // of even and of odd codes
+    for (int g = first >> 2; g <= last_group; g += 16) {
+      uint32_t w[16];
+#pragma unroll
+      for (int q = 0; q < 16; ++q) w[q] = g + q <= last_group ? codes[g + q] : 0u;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        if (4 * (g + q) + 4 > steps) w[q] &= (1u << (8 * (steps & 3))) - 1u;
+        most = pk_max(most, pk_max(w[q] & 0x00ff00ffu, w[q] >> 8 & 0x00ff00ffu));
+      }
+    }
+    const int top = static_cast<int>(max(most & 0xffffu, most >> 16));
+    tops[t] = top == 255 ? 0 : top - 127;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) top_a[i] = tops[wm + 32 * i + (lane & 31)];
+#pragma unroll
+    for (int j = 0; j < kTN; ++j) top_b[j] = tops[kBM + wn + 32 * j + (lane & 31)];
     wait_loads<kLoads>();
     if (tail && first + 1 == steps) clear_slot(0);
-    read_codes(first, ca, cb);
+    read_scales(first, sa, sb);
 #pragma unroll
     for (int i = 0; i < kParts; ++i) read_part(0, 0, i);
   }
@@ -313,7 +335,7 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
 #pragma unroll
         for (int i = g.value * kLoads / kIssue; i < (g.value + 1) * kLoads / kIssue; ++i) {
           if (i < 2 * kParts) load_rows(ahead, slot, i);
-          else load_codes(min((kt >> 2) + 1, last_group), kCodeUnits == 1 ? 0 : kt & 1);
+          else load_codes(min((kt >> 2) + 1, last_group));
         }
     };
     for_parts<kParts>([&](auto g) {
@@ -323,61 +345,63 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
       }
       if constexpr (g.value == kOpen || g.value == kOpenB) wait_reads();
       issue(Part<g.value - kOpen>{});
-      mma<PRECISE, g.value>(xa[0], ca, yb[0], cb, acc, cvt);
+      mma<g.value>(xa[0], sa, yb[0], sb, acc, cvt);
       __builtin_amdgcn_sched_barrier(0);
     });
-    int na[TM], nb[TN];
+    float na[kTM], nb[kTN];
     for_parts<kParts>([&](auto g) {
       // loads of step kt + 2 issued before this group
       constexpr int issued = (kParts + g.value - kOpen) * kLoads / kIssue;
       if constexpr (g.value == 0) {
-        wait_loads<kLoads - 2 * TM + issued>();
+        wait_loads<kLoads - 2 * kTM + issued>();
         if (tail && kt + 2 == steps) clear_slot(next);
-        read_codes(kt + 1, na, nb);
+        read_scales(kt + 1, na, nb);
       }
-      if constexpr (g.value == TM) wait_loads<issued>();
+      if constexpr (g.value == kTM) wait_loads<issued>();
       read_part(next, 0, g.value);
       issue(Part<kParts + g.value - kOpen>{});
-      mma<PRECISE, g.value>(xa[1], ca, yb[1], cb, acc, cvt);
+      mma<g.value>(xa[1], sa, yb[1], sb, acc, cvt);
       __builtin_amdgcn_sched_barrier(0);
     });
 #pragma unroll
-    for (int i = 0; i < TM; ++i) ca[i] = na[i];
+    for (int i = 0; i < kTM; ++i) sa[i] = na[i];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) cb[j] = nb[j];
+    for (int j = 0; j < kTN; ++j) sb[j] = nb[j];
     slot = next;
   }
   wait_loads<0>();  // nothing lands in LDS from here on
 
   // A lane holds 4 consecutive columns of a row at a time; through LDS, 32
   // rows of the wave's tile at a time, the rows become contiguous.
-  typedef typename std::conditional<PRECISE || PART, float, uint16_t>::type Out;
   constexpr int kPer = 16 / sizeof(Out);             // elements of a 16-byte store
-  constexpr int kPitch = WN + kPer;
+  constexpr int kPitch = kWN + kPer;
   static_assert(4 * 32 * kPitch * sizeof(Out) <= 2 * kSlot, "the waves' slabs fit the slots");
   Out* const slab = reinterpret_cast<Out*>(lds) + wave * 32 * kPitch;
   Out* const out = static_cast<Out*>(p.out) + (PART ? blockIdx.y * p.m * p.ld_out : 0) +
                    (m0 + wm) * p.ld_out + n0 + wn;
   const int64_t rows = p.m - m0 - wm, cols = p.n - n0 - wn;
+  const bool any = first < steps;  // else the sums are zeros, of no scale
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
+  for (int i = 0; i < kTM; ++i) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < kTN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
         Out* const q = slab + (lane & 31) * kPitch + 32 * j + 2 * e + 4 * (lane >> 5);
-        if constexpr (sizeof(Out) == 4) {
-          *reinterpret_cast<v4f*>(q) = v4f{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-        } else {
-          const v4b v = __builtin_convertvector(
-              (v4f{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]}), v4b);
-          *reinterpret_cast<v4b*>(q) = v;
+        v4f v = {acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+        if (any) {
+          const v4i top =
+              *reinterpret_cast<const v4i*>(tops + kBM + wn + 32 * j + 2 * e + 4 * (lane >> 5));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[c] = __builtin_ldexpf(v[c], top_a[i] + top[c]);
         }
+        if constexpr (sizeof(Out) == 4) *reinterpret_cast<v4f*>(q) = v;
+        else *reinterpret_cast<v4b*>(q) = __builtin_convertvector(v, v4b);
       }
     __builtin_amdgcn_wave_barrier();
-    constexpr int kRun = WN / kPer, kStep = 64 / kRun;  // lanes of a row, rows of a store
+    constexpr int kRun = kWN / kPer, kStep = 64 / kRun;  // lanes of a row, rows of a store
     const int c = lane % kRun * kPer;
-    if (rows >= 32 * (i + 1) && cols >= WN) {
+    if (rows >= 32 * (i + 1) && cols >= kWN) {
 #pragma unroll
       for (int r = 0; r < 32; r += kStep) {
         const int rr = r + lane / kRun;
@@ -436,8 +460,9 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const float* __restric
 // registers, and little else counts.  A block takes 16 rows of b; its waves take
 // shares of the reduction, each with the loads of U steps in flight, and their
 // sums are added in order.  a's rows past its end repeat the last one.  16 x 16
-// products: b's rows along the accumulator's registers, a's along its lanes.
-template <int W, int U, bool PRECISE>
+// products: b's rows along the accumulator's registers, a's along its lanes.  Each
+// group's sum is multiplied by its scales, in fp32.
+template <int W, int U, typename Out>
 __global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p) {
   __shared__ float sums[W][4][64];
   const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6);
@@ -481,16 +506,16 @@ __global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p) {
         }
       }
       const v8i x = join(a[u][0], a[u][1]), y = join(b[u][0], b[u][1]);
-      if constexpr (!PRECISE) {
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(y, x, acc, 0, 0, 0, cb[u], 0, ca[u]);
-      } else {
-        v8b xb[4], yb[4];
-        to_bf16(x, ca[u], xb);
-        to_bf16(y, cb[u], yb);
+      v8b xb[4], yb[4];
+      to_bf16(x, ca[u] == 255 ? __uint_as_float(255u << 23) : 1.0f, xb);
+      to_bf16(y, cb[u] == 255 ? __uint_as_float(255u << 23) : 1.0f, yb);
+      v4f sum = {0, 0, 0, 0};
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yb[q], xb[q], acc, 0, 0, 0);
-      }
+      for (int q = 0; q < 4; ++q)
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yb[q], xb[q], sum, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        acc[e] += __builtin_ldexpf(sum[e], ca[u] + __shfl(cb[u], 4 * g + e) - 254);
     }
   }
 #pragma unroll
@@ -504,7 +529,7 @@ __global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p) {
     for (int w = 1; w < W; ++w) v += sums[w][e][l];
     if (row < p.m && n0 + col < p.n) {
       const int64_t at = row * p.ld_out + n0 + col;
-      if constexpr (PRECISE) static_cast<float*>(p.out)[at] = v;
+      if constexpr (sizeof(Out) == 4) static_cast<float*>(p.out)[at] = v;
       else static_cast<uint16_t*>(p.out)[at] = round_bf16(v);
     }
   }
@@ -518,26 +543,22 @@ constexpr int64_t kRowsMax = 16;
 constexpr int64_t kRowsReach = int64_t(1) << 27;
 bool takes_rows(int64_t m, int64_t n) { return m <= kRowsMax && n <= kRowsReach; }
 
-int64_t tiles(const int64_t m, const int64_t n, int bm, int bn) {
-  return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
-}
+int64_t tiles(int64_t m, int64_t n) { return ((m + kBM - 1) / kBM) * ((n + kBN - 1) / kBN); }
 
-// Shares of the reduction where 128 x 128 tiles do not fill the 256 CUs: the
-// number for which this estimate in us is least.  A step takes 0.42 us on a CU
-// of its own and 0.58 as one of two (precise 0.95 and 1.75); a share's partial
-// result is written and read at some 6 TB/s, the joining launch costs 3.  E.g.
-// 512 x 1024 x 11008: 1 share 41 us, 8 shares 20.6; 256 x 4096 x 4096 18.1, 17.1.
-int shares(int64_t m, int64_t n, int64_t k, bool precise) {
+// Shares of the reduction where the tiles do not fill the 256 CUs: the number for
+// which this estimate in us is least.  A step takes 0.95 us on a CU of its own and
+// 1.75 as one of two; a share's partial result is written and read at some 6 TB/s,
+// the joining launch costs 3.
+int shares(int64_t m, int64_t n, int64_t k) {
   if (takes_rows(m, n)) return 1;
-  const int64_t t = tiles(m, n, 128, 128), steps = (k + kBK - 1) / kBK;
+  const int64_t t = tiles(m, n), steps = (k + kBK - 1) / kBK;
   if (t > 160) return 1;
   int best = 1;
   double least = 1e30;
   for (int s = 1; s <= 16 && s * t <= 512; ++s) {
     const int64_t per = ((steps + s - 1) / s + 3) / 4 * 4;  // (codes come four steps at a time)
     if (s > 1 && (s - 1) * per >= steps) continue;
-    const double step = s * t > 256 ? (precise ? 1.75 : 0.58) : (precise ? 0.95 : 0.42);
-    const double us = per * step + (s > 1 ? 3.0 + 8.0 * s * m * n / 6e6 : 0.0);
+    const double us = per * (s * t > 256 ? 1.75 : 0.95) + (s > 1 ? 3.0 + 8.0 * s * m * n / 6e6 : 0.0);
     if (us < least) {
       least = us;
       best = s;
@@ -546,10 +567,10 @@ int shares(int64_t m, int64_t n, int64_t k, bool precise) {
   return best;
 }
 
-template <bool PRECISE>
+template <typename Out>
 void launch_rows(const MatmulArgs& a, hipStream_t s) {
 #define ZF_ROWS(W, U)                                                                   \
-  hipLaunchKernelGGL((matmul_rows_kernel<W, U, PRECISE>), dim3(static_cast<uint32_t>(blocks)), \
+  hipLaunchKernelGGL((matmul_rows_kernel<W, U, Out>), dim3(static_cast<uint32_t>(blocks)), \
                      dim3(64 * W), 0, s, a)
   const int64_t blocks = (a.n + 15) / 16;
   if (blocks >= 512) ZF_ROWS(4, 8);
@@ -558,66 +579,41 @@ void launch_rows(const MatmulArgs& a, hipStream_t s) {
 #undef ZF_ROWS
 }
 
-template <bool PRECISE>
+template <typename Out>
 void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
-#define ZF_TILES(BM, BN, PART, Y, ARGS)                                                          \
-  hipLaunchKernelGGL((matmul_tile_kernel<BM, BN, PRECISE, PART>),                                \
-                     dim3(static_cast<uint32_t>(tiles(a.m, a.n, BM, BN)), Y), dim3(256), 0, s, ARGS)
-  // Larger tiles ask less of the memory system and take longer to fill the
-  // chip.  Us with 256 x 256 / 128 x 256 / 128 x 128 tiles: 8192 x 4096 x 11008 285 /
-  // 352 / 402, 1024 x 11008 x 4096 (172 / 344 / 688 tiles) 49 / 58 / 52, 2048 x
-  // 4096 x 11008 (128 / 256 / 512) 118 / 92 / 104, 1024 x 4096 x 4096 (64 / 128 /
-  // 256) 44 / 29 / 24.  The precise form is bound by its products: 128 x 256 and
-  // 128 x 128 within 2% from 2048 x 4096 x 4096 on, 48 / 45 at 1003 x 5003 x 3001;
-  // 128 x 192 46 there and 296, not 236, at 8192 x 4096 x 4096.
-  if constexpr (!PRECISE) {
-    if (tiles(a.m, a.n, 256, 256) >= 160) {
-      ZF_TILES(256, 256, false, 1, a);
-      return;
-    }
-    if (tiles(a.m, a.n, 128, 256) >= 160) {
-      ZF_TILES(128, 256, false, 1, a);
-      return;
-    }
+  const dim3 grid(static_cast<uint32_t>(tiles(a.m, a.n)));
+  const int q = shares(a.m, a.n, a.k);
+  if (q == 1) {
+    hipLaunchKernelGGL((matmul_tile_kernel<Out, false>), grid, dim3(256), 0, s, a);
+    return;
   }
-  if (const int q = shares(a.m, a.n, a.k, PRECISE); q > 1) {
-    MatmulArgs b = a;
-    b.out = ws;
-    b.ld_out = a.n;
-    const int64_t steps = (a.k + kBK - 1) / kBK;
-    b.share = static_cast<int32_t>(((steps + q - 1) / q + 3) / 4 * 4);
-    ZF_TILES(128, 128, true, q, b);
-    const int64_t blocks = (a.m * a.n + 2047) / 2048;
-    const dim3 grid(static_cast<uint32_t>(blocks < 2048 ? blocks : 2048));
-    if (PRECISE)
-      hipLaunchKernelGGL((matmul_join_kernel<float>), grid, dim3(256), 0, s,
-                         static_cast<const float*>(ws), q, a.m, a.n, static_cast<float*>(a.out),
-                         a.ld_out);
-    else
-      hipLaunchKernelGGL((matmul_join_kernel<uint16_t>), grid, dim3(256), 0, s,
-                         static_cast<const float*>(ws), q, a.m, a.n, static_cast<uint16_t*>(a.out),
-                         a.ld_out);
-  } else {
-    ZF_TILES(128, 128, false, 1, a);
-  }
-#undef ZF_TILES
+  MatmulArgs b = a;
+  b.out = ws;
+  b.ld_out = a.n;
+  const int64_t steps = (a.k + kBK - 1) / kBK;
+  b.share = static_cast<int32_t>(((steps + q - 1) / q + 3) / 4 * 4);
+  hipLaunchKernelGGL((matmul_tile_kernel<float, true>), dim3(grid.x, q), dim3(256), 0, s, b);
+  const int64_t blocks = (a.m * a.n + 2047) / 2048;
+  hipLaunchKernelGGL((matmul_join_kernel<Out>), dim3(static_cast<uint32_t>(std::min<int64_t>(blocks, 2048))),
+                     dim3(256), 0, s, static_cast<const float*>(ws), q, a.m, a.n,
+                     static_cast<Out*>(a.out), a.ld_out);
 }
 
 }  // namespace
 
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k) {
-  const int q = std::max(shares(m, n, k, false), shares(m, n, k, true));
+  const int q = shares(m, n, k);
   return q > 1 ? static_cast<size_t>(q) * m * n * sizeof(float) : 0;
 }
 
 hipError_t launch_matmul(const MatmulArgs& a, void* ws, hipStream_t s) {
   (void)hipGetLastError();
   if (takes_rows(a.m, a.n)) {
-    if (a.out_f32) launch_rows<true>(a, s);
-    else launch_rows<false>(a, s);
+    if (a.out_f32) launch_rows<float>(a, s);
+    else launch_rows<uint16_t>(a, s);
   } else {
-    if (a.out_f32) launch_tiles<true>(a, ws, s);
-    else launch_tiles<false>(a, ws, s);
+    if (a.out_f32) launch_tiles<float>(a, ws, s);
+    else launch_tiles<uint16_t>(a, ws, s);
   }
   return hipGetLastError();
 }
