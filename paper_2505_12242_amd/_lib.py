@@ -8,6 +8,7 @@ module raises if libzf.so has not been built -- there is no fallback.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -219,6 +220,22 @@ def _stream(stream) -> Optional[int]:
     # torch.cuda.current_stream().cuda_stream without the Stream object (looked
     # up here: a torch without a GPU backend has neither name)
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _on(stream):
+    """Context for what a call launched on `stream` (a torch stream; None: the
+    current one) allocates.  A block of torch's allocator belongs to the stream
+    that is current when it is allocated: only there may it be used before its
+    last owner's work is done, and be handed on while its own still runs."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
+    """torch.empty for a call launched on `stream` (see _on)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _mat(t: torch.Tensor, dtype, name: str, rows: Optional[int] = None,
@@ -450,11 +467,11 @@ def colnorm(grad: torch.Tensor, out: Optional[torch.Tensor] = None,
     n, m = _logical(grad, layout)
     ld = _mat(grad, torch.bfloat16, "grad")
     if out is None:
-        out = torch.empty(m, dtype=torch.float32, device=grad.device)
+        out = _empty(m, torch.float32, grad.device, stream)
     _vec(out, torch.float32, "out", m)
     if workspace is None:
         need = colnorm_workspace_bytes(n, m, layout)
-        workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=grad.device)
+        workspace = _empty(max(need, 8), torch.uint8, grad.device, stream)
     _check("zf_colnorm", LIB.zf_colnorm(_ptr(grad), n, m, ld, layout, _ptr(out),
                                         _ptr(workspace), workspace.numel(), _stream(stream)))
     return out
@@ -500,7 +517,8 @@ def topk_select(norms: torch.Tensor, ratio: float, out: Optional[Selection] = No
     k = k_from_ratio(ratio, m)
     _vec(norms, torch.float32, "norms", m)
     if out is None:
-        out = Selection(m, k, norms.device)
+        with _on(stream):
+            out = Selection(m, k, norms.device)
     if out.m != m or out.k != k:
         raise ValueError(f"selection buffers are for m={out.m}, k={out.k}; need m={m}, k={k}")
     c_sel = out.as_c()
@@ -623,7 +641,8 @@ def update_fused_handover(grad, sel: Selection, master, exp_avg, exp_avg_sq, wei
     ldw = _lmat(weight, torch.bfloat16, "weight", layout, n, m)
     lda = _lmat(acc, torch.float32, "acc", layout, n, m - sel.k)
     if out is None:
-        out = alloc_stored(layout, n, m, torch.float32, grad.device)
+        with _on(stream):
+            out = alloc_stored(layout, n, m, torch.float32, grad.device)
     ldo = _lmat(out, torch.float32, "out", layout, n, m)
     c_sel, c_hp = sel.as_c(), hp.as_c()
     c_src = src.as_c() if src is not None else None
@@ -641,7 +660,8 @@ def unpack(acc, sel: Selection, scale: float = 1.0, out: Optional[torch.Tensor] 
     n = acc.shape[0] if layout == ROW_MAJOR else acc.shape[1]
     lda = _lmat(acc, torch.float32, "acc", layout, n, m - sel.k)
     if out is None:
-        out = alloc_stored(layout, n, m, torch.float32, acc.device)
+        with _on(stream):
+            out = alloc_stored(layout, n, m, torch.float32, acc.device)
     ldo = _lmat(out, torch.float32, "out", layout, n, m)
     c_sel = sel.as_c()
     _check("zf_unpack", LIB.zf_unpack(_ptr(acc), lda, ctypes.byref(c_sel), sel.k, n, m, layout,
@@ -804,7 +824,7 @@ class Plan:
             dev = torch.device("cuda", torch.cuda.current_device())
         self.device = dev
         # 256-byte aligned start inside the buffer
-        self._mem = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=dev)
+        self._mem = _empty(nbytes.value + 256, torch.uint8, dev, stream)
         base = self._mem.data_ptr()
         aligned = (base + 255) & ~255
         st = stream if stream is not None else torch.cuda.current_stream(dev)

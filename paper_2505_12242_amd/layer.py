@@ -4,6 +4,11 @@ selective update serves.
 Argument marshalling only, as in _lib.py: tensors are checked for dtype,
 device, shape and stride, outputs that are not given are allocated, and every
 operator runs in the HIP kernels of libzf.so.
+
+`stream` is the torch stream a call is launched on (None: the current one).  What
+the call allocates, outputs and workspaces, belongs to that stream; the inputs
+must be ready there, and an output that is used on another stream is the
+caller's to order, as any tensor's.
 """
 
 from __future__ import annotations
@@ -14,8 +19,8 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
-from ._lib import (LIB, AdamHparams, ZfAdamwTensor, ZfFp8, _check, _mat, _ptr, _stream, _vec,
-                   c_sz, c_vp)
+from ._lib import (LIB, AdamHparams, ZfAdamwTensor, ZfFp8, _check, _empty, _mat, _ptr, _stream,
+                   _vec, c_sz, c_vp)
 
 DTYPES = {torch.bfloat16: 0, torch.float32: 1}  # zf_dtype
 DATA, SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
@@ -90,12 +95,12 @@ class Fp8:
                              f"rows)")
 
 
-def _alloc_fp8(rows: int, cols: int, group: int, device) -> Tuple[Fp8, ZfFp8]:
+def _alloc_fp8(rows: int, cols: int, group: int, device, stream=None) -> Tuple[Fp8, ZfFp8]:
     """A new Fp8 and its C struct."""
     sr, sc = -(-rows // group), -(-cols // 128)
     ld, ld_scale = _up(cols, 16), _up(sc, 4)
-    data = torch.empty((rows, ld), dtype=DATA, device=device)
-    scale = torch.empty((sr, ld_scale), dtype=SCALE, device=device)
+    data = _empty((rows, ld), DATA, device, stream)
+    scale = _empty((sr, ld_scale), SCALE, device, stream)
     c = ZfFp8(data.data_ptr() or None, ld, scale.data_ptr() or None, ld_scale, group)
     if ld != cols:
         data = data[:, :cols]
@@ -122,11 +127,11 @@ def quantize_fp8(x: torch.Tensor, group: int = 1, rows: bool = True, transposed:
     if out is not None:
         c_out = out.as_c("out", r, c)
     elif rows:
-        out, c_out = _alloc_fp8(r, c, group, x.device)
+        out, c_out = _alloc_fp8(r, c, group, x.device, stream)
     if out_t is not None:
         c_out_t = out_t.as_c("out_t", c, r)
     elif transposed:
-        out_t, c_out_t = _alloc_fp8(c, r, group, x.device)
+        out_t, c_out_t = _alloc_fp8(c, r, group, x.device, stream)
     if out is None and out_t is None:
         raise ValueError("neither output is wanted")
     _check("zf_quantize_fp8", LIB.zf_quantize_fp8(
@@ -150,13 +155,13 @@ def matmul_fp8(a: Fp8, b: Fp8, out: Optional[torch.Tensor] = None, dtype=torch.b
     n = b.data.shape[0]
     c_a, c_b = a.as_c("a"), b.as_c("b", None, k)
     if out is None:
-        out, ld = torch.empty((m, n), dtype=dtype, device=a.data.device), n
+        out, ld = _empty((m, n), dtype, a.data.device, stream), n
     else:
         ld = _mat(out, out.dtype, "out", m, n)
     dt = _dtype(out, "out")
     need = LIB.zf_matmul_fp8_workspace_bytes(m, n, k)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
+        workspace = _empty(need, torch.uint8, out.device, stream)
     _check("zf_matmul_fp8", LIB.zf_matmul_fp8(
         ctypes.byref(c_a), ctypes.byref(c_b), m, n, k, _ptr(out), dt, ld, _ptr(workspace),
         0 if workspace is None else workspace.numel() * workspace.element_size(),
@@ -191,7 +196,7 @@ def rmsnorm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tensor
     _vec(gain, gain.dtype, "gain", c)
     dtype, dev = x.dtype, x.device
     if rstd is None:
-        rstd = torch.empty(r, dtype=torch.float32, device=dev)
+        rstd = _empty(r, torch.float32, dev, stream)
     else:
         _vec(rstd, torch.float32, "rstd", r)
     ld_res, ld_h, ld_y, c_q = 0, c, c, None
@@ -200,15 +205,15 @@ def rmsnorm(x: torch.Tensor, gain: torch.Tensor, residual: Optional[torch.Tensor
     if h is not None:
         ld_h = _mat(h, dtype, "h", r, c)
     elif residual is not None:
-        h = torch.empty((r, c), dtype=dtype, device=dev)
+        h = _empty((r, c), dtype, dev, stream)
     if y is not None:
         ld_y = _mat(y, dtype, "y", r, c)
     elif want_y:
-        y = torch.empty((r, c), dtype=dtype, device=dev)
+        y = _empty((r, c), dtype, dev, stream)
     if q is not None:
         c_q = q.as_c("q", r, c)
     elif want_q:
-        q, c_q = _alloc_fp8(r, c, 1, dev)
+        q, c_q = _alloc_fp8(r, c, 1, dev, stream)
     _check("zf_rmsnorm_forward", LIB.zf_rmsnorm_forward(
         _ptr(x), ld, _ptr(residual), ld_res, dt, r, c, _ptr(gain), gdt, float(eps), _ptr(h), ld_h,
         _ptr(y), ld_y, ctypes.byref(c_q) if c_q is not None else None, _ptr(rstd),
@@ -240,17 +245,17 @@ def rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd
     if dresidual is not None:
         ld_res = _mat(dresidual, dy.dtype, "dresidual", r, c)
     if dx is None:
-        dx, ld_dx = torch.empty((r, c), dtype=dy.dtype, device=dy.device), c
+        dx, ld_dx = _empty((r, c), dy.dtype, dy.device, stream), c
     else:
         ld_dx = _mat(dx, dy.dtype, "dx", r, c)
     if dgain is not None:
         _vec(dgain, torch.float32, "dgain", c)
     elif want_dgain:
-        dgain = torch.empty(c, dtype=torch.float32, device=dy.device)
+        dgain = _empty(c, torch.float32, dy.device, stream)
     if dgain is not None:
         if workspace is None:
             need = LIB.zf_rmsnorm_backward_workspace_bytes(r, c)
-            workspace = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+            workspace = _empty(need, torch.uint8, dy.device, stream) if need else None
     _check("zf_rmsnorm_backward", LIB.zf_rmsnorm_backward(
         _ptr(dy), ld_dy, _ptr(h), ld_h, dt, r, c, _ptr(gain), gdt, _ptr(rstd), _ptr(dresidual),
         ld_res, _ptr(dx), ld_dx, _ptr(dgain), _ptr(workspace),
@@ -337,7 +342,7 @@ class AdamWPlan:
         _check("zf_adamw_plan_query",
                LIB.zf_adamw_plan_query(arr, len(self.tensors), ctypes.byref(nbytes)))
         self.device = self.tensors[0].master.device
-        self._mem = torch.empty(nbytes.value + 256, dtype=torch.uint8, device=self.device)
+        self._mem = _empty(nbytes.value + 256, torch.uint8, self.device, stream)
         aligned = (self._mem.data_ptr() + 255) & ~255
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
         h = c_vp()
