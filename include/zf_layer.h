@@ -104,7 +104,8 @@ zf_status zf_matmul_fp8(const zf_fp8* a, const zf_fp8* b, int64_t m, int64_t n, 
  * arithmetic in fp32.  h is required with a residual and may be x or the
  * residual itself (the same address and stride).  y and q may each be NULL;
  * q receives y in 8 bits (group 1).  rstd: [rows] fp32, required (the
- * backward pass reads it).  eps finite and >= 0.  rows, cols < 2^30. */
+ * backward pass reads it); with cols = 0 it is 1 / sqrt(eps).  eps finite and
+ * >= 0.  rows, cols < 2^30. */
 zf_status zf_rmsnorm_forward(const void* x, int64_t ld_x, const void* residual,
                              int64_t ld_residual, int32_t dtype, int64_t rows, int64_t cols,
                              const void* gain, int32_t gain_dtype, double eps, void* h,

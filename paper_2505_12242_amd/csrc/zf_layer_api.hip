@@ -179,7 +179,7 @@ zf_status zf_rmsnorm_forward(const void* x, int64_t ld_x, const void* residual,
   if ((overlaps(sh, sx) && (h != x || (rows > 1 && ld_h != ld_x))) ||
       (overlaps(sh, sr) && (h != residual || (rows > 1 && ld_h != ld_residual))))
     return ZF_EINVAL;
-  if (rows == 0 || cols == 0) return ZF_OK;
+  if (rows == 0) return ZF_OK;
   const zf::NormArgs a{x, ld_x, residual, ld_residual, rows, cols, gain, gain_dtype == ZF_F32,
                        static_cast<float>(eps), h, ld_h, y, ld_y, fp8_out(q), rstd};
   return done(zf::launch_rmsnorm(a, dtype, as_stream(stream)));

@@ -91,6 +91,11 @@ __device__ __forceinline__ void store_y(const NormArgs& a, int64_t row, int64_t 
   }
 }
 
+// The mean of `cols` squares; a row without elements counts as one of zeros.
+__device__ __forceinline__ float mean_square(float sum, int64_t cols) {
+  return sum / static_cast<float>(cols > 0 ? cols : 1);
+}
+
 // RES: a residual is added (and h written); without one h may still be wanted.
 // (8 waves to a SIMD, which the scalar registers would else leave at 7: 8192 x 5120
 // 64 us, not 73.)
@@ -122,7 +127,7 @@ __global__ __launch_bounds__(NT, V == 1 ? 8 : 1) void rmsnorm_kernel(NormArgs a)
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss += h[i][j] * h[i][j];
     }
-    const float mean = block_sum<NT>(ss, red[flip]) / static_cast<float>(a.cols);
+    const float mean = mean_square(block_sum<NT>(ss, red[flip]), a.cols);
     flip ^= 1;
     const float rstd = 1.0f / sqrtf(mean + a.eps);
     if (threadIdx.x == 0) a.rstd[row] = rstd;
@@ -151,7 +156,7 @@ __global__ __launch_bounds__(NT) void rmsnorm_wide_kernel(NormArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss += h[j] * h[j];
     }
-    const float mean = block_sum<NT>(ss, red[flip]) / static_cast<float>(a.cols);
+    const float mean = mean_square(block_sum<NT>(ss, red[flip]), a.cols);
     flip ^= 1;
     const float rstd = 1.0f / sqrtf(mean + a.eps);
     if (threadIdx.x == 0) a.rstd[row] = rstd;
