@@ -259,12 +259,10 @@ def _mat(t: torch.Tensor, dtype, name: str, rows: Optional[int] = None,
     elif not host and r and c and not (device_ok and t.is_pinned()):
         raise ValueError(f"{name}: must live on a GPU" +
                          (" or in pinned host memory" if device_ok else ""))
-    if r <= 1:
-        return c
     ld, step = t.stride()
-    if c > 1 and step != 1:
+    if step != 1 and c > 1 and r:
         raise ValueError(f"{name}: rows must be contiguous (stride(1) == 1)")
-    return ld
+    return ld if r > 1 else c
 
 
 def _logical(t: torch.Tensor, layout: int):
