@@ -265,6 +265,15 @@ def _mat(t: torch.Tensor, dtype, name: str, rows: Optional[int] = None,
     return ld if r > 1 else c
 
 
+def _workspace(t: Optional[torch.Tensor]) -> int:
+    """Checks a workspace, of any type and shape, and returns its bytes."""
+    if t is None:
+        return 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace: must be a contiguous GPU tensor")
+    return t.numel() * t.element_size()
+
+
 def _logical(t: torch.Tensor, layout: int):
     """(n, m) of a matrix stored as tensor t in `layout`."""
     if layout not in (ROW_MAJOR, CHANNEL_MAJOR):
@@ -471,7 +480,7 @@ def colnorm(grad: torch.Tensor, out: Optional[torch.Tensor] = None,
         need = colnorm_workspace_bytes(n, m, layout)
         workspace = _empty(max(need, 8), torch.uint8, grad.device, stream)
     _check("zf_colnorm", LIB.zf_colnorm(_ptr(grad), n, m, ld, layout, _ptr(out),
-                                        _ptr(workspace), workspace.numel(), _stream(stream)))
+                                        _ptr(workspace), _workspace(workspace), _stream(stream)))
     return out
 
 

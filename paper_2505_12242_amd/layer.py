@@ -20,7 +20,7 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 import torch
 
 from ._lib import (LIB, AdamHparams, ZfAdamwTensor, ZfFp8, _check, _empty, _mat, _ptr, _stream,
-                   _vec, c_sz, c_vp)
+                   _vec, _workspace, c_sz, c_vp)
 
 DTYPES = {torch.bfloat16: 0, torch.float32: 1}  # zf_dtype
 DATA, SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
@@ -164,8 +164,7 @@ def matmul_fp8(a: Fp8, b: Fp8, out: Optional[torch.Tensor] = None, dtype=torch.b
         workspace = _empty(need, torch.uint8, out.device, stream)
     _check("zf_matmul_fp8", LIB.zf_matmul_fp8(
         ctypes.byref(c_a), ctypes.byref(c_b), m, n, k, _ptr(out), dt, ld, _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(),
-        _stream(stream)))
+        _workspace(workspace), _stream(stream)))
     return out
 
 
@@ -259,8 +258,7 @@ def rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd
     _check("zf_rmsnorm_backward", LIB.zf_rmsnorm_backward(
         _ptr(dy), ld_dy, _ptr(h), ld_h, dt, r, c, _ptr(gain), gdt, _ptr(rstd), _ptr(dresidual),
         ld_res, _ptr(dx), ld_dx, _ptr(dgain), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(),
-        _stream(stream)))
+        _workspace(workspace), _stream(stream)))
     return dx, dgain
 
 

@@ -20,3 +20,10 @@ def test_a_single_rows_elements_are_contiguous(t):
                                torch.zeros(8, 0).t()[:0], torch.zeros(0, 4)], ids=str)
 def test_a_single_row_needs_no_row_stride(t):
     assert _lib._mat(t, torch.float32, "x", host=True) == t.shape[1]
+
+
+def test_workspace_is_on_the_gpu():
+    """A workspace in host memory is refused before the kernels would write to it."""
+    assert _lib._workspace(None) == 0
+    with pytest.raises(ValueError, match="workspace"):
+        _lib._workspace(torch.empty(64, dtype=torch.uint8))
