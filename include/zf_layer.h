@@ -163,7 +163,8 @@ typedef struct zf_adamw_plan zf_adamw_plan;
 /* Device bytes of a plan over these tensors (its tables).  tensors: HOST
  * array of count >= 1; 32- and 8-bit states and both gradient types may be
  * mixed.  Every pointer is aligned to its element; no two buffers overlap.
- * Together fewer than 2^34 elements (one launch). */
+ * One launch takes fewer than 2^24 blocks of 1024 elements, a tensor's last one
+ * partly filled: the sum of ceil(n / 1024) over the tensors is below 2^24. */
 zf_status zf_adamw_plan_query(const zf_adamw_tensor* tensors, int32_t count,
                               size_t* device_bytes);
 
