@@ -6,11 +6,11 @@
 // instruction, and why).
 //
 // Three forms.  Many rows: tiles of 128 x 128 (matmul_tile_kernel), bound by the
-// bf16 instruction's rate and the conversions before it: 1.12-1.16 PFLOP/s at 8192 x
+// bf16 instruction's rate and the conversions before it: 1.15-1.20 PFLOP/s at 8192 x
 // 11008 x 4096, 8192 x 4096 x 11008, 4096 x 11008 x 8192 and 2048 x 4096 x 11008.  Few
 // tiles: the reduction is split over blocks and the shares' results joined in order
 // (64 x 11008 x 4096: 22 + 4 us).  Up to 16 rows: the second operand's bytes are all
-// that counts (matmul_rows_kernel; 1 x 11008 x 4096: 45 MB in 11.5 us, 4.0 TB/s).
+// that counts (matmul_rows_kernel; 1 x 11008 x 4096: 45 MB in 11.8 us, 3.8 TB/s).
 #include <algorithm>
 
 #include "zf_layer.hpp"
@@ -21,9 +21,7 @@ namespace {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
-typedef int v4i __attribute__((ext_vector_type(4)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
-typedef __bf16 v4b __attribute__((ext_vector_type(4)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 
 constexpr int kBK = 128;  // reduction per step: one scale group
@@ -297,21 +295,17 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
     load_step(first, 0);
     load_step(min(first + 1, steps - 1), 1);
     load_codes(min((first >> 2) + 1, last_group));
-    // The thread's row's largest code less 127, 64 codes at a time (what follows
-    // the last step's may be anything).  With a NaN's among them, 0: it stays one.
+    // The thread's row's largest code less 127 (what follows the last step's in its
+    // word may be anything).  With a NaN's among them, 0: it stays one.
     const uint32_t* const codes = reinterpret_cast<const uint32_t*>(
         t < kBM ? p.a.scale + (m0 >> p.a.shift) * p.a.ld_scale + code_row
                 : p.b.scale + (n0 >> p.b.shift) * p.b.ld_scale + code_row);
     uint32_t most = 0;  // of even and of odd codes
-    for (int g = first >> 2; g <= last_group; g += 16) {
-      uint32_t w[16];
-#pragma unroll
-      for (int q = 0; q < 16; ++q) w[q] = g + q <= last_group ? codes[g + q] : 0u;
-#pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        if (4 * (g + q) + 4 > steps) w[q] &= (1u << (8 * (steps & 3))) - 1u;
-        most = pk_max(most, pk_max(w[q] & 0x00ff00ffu, w[q] >> 8 & 0x00ff00ffu));
-      }
+    const uint32_t whole = steps & 3 ? (1u << (8 * (steps & 3))) - 1u : ~0u;  // of the last word
+#pragma unroll 8
+    for (int g = first >> 2; g <= last_group; ++g) {
+      const uint32_t w = codes[g] & (g == last_group ? whole : ~0u);
+      most = pk_max(most, pk_max(w & 0x00ff00ffu, w >> 8 & 0x00ff00ffu));
     }
     const int top = static_cast<int>(max(most & 0xffffu, most >> 16));
     tops[t] = top == 255 ? 0 : top - 127;
@@ -372,47 +366,49 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   wait_loads<0>();  // nothing lands in LDS from here on
 
   // A lane holds 4 consecutive columns of a row at a time; through LDS, 32
-  // rows of the wave's tile at a time, the rows become contiguous.
-  constexpr int kPer = 16 / sizeof(Out);             // elements of a 16-byte store
-  constexpr int kPitch = kWN + kPer;
-  static_assert(4 * 32 * kPitch * sizeof(Out) <= 2 * kSlot, "the waves' slabs fit the slots");
-  Out* const slab = reinterpret_cast<Out*>(lds) + wave * 32 * kPitch;
+  // rows of the wave's tile at a time, the rows become contiguous.  (Scaled on their
+  // way out, in a loop: as they are written, each of 64 results in code of its own,
+  // 256 x 4096 x 4096 took 23.2 us, not 22.2.)
+  constexpr int kPitch = kWN + 4;
+  static_assert(4 * 32 * kPitch * 4 <= 2 * kSlot, "the waves' slabs fit the slots");
+  float* const slab = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
+  constexpr int kPer = 16 / sizeof(Out), kRun = kWN / kPer;  // elements of a store, lanes of a row
+  const int c = lane % kRun * kPer;
   Out* const out = static_cast<Out*>(p.out) + (PART ? blockIdx.y * p.m * p.ld_out : 0) +
-                   (m0 + wm) * p.ld_out + n0 + wn;
-  const int64_t rows = p.m - m0 - wm, cols = p.n - n0 - wn;
-  const bool any = first < steps;  // else the sums are zeros, of no scale
+                   (m0 + wm) * p.ld_out + n0 + wn + c;
+  const int64_t rows = p.m - m0 - wm, cols = p.n - n0 - wn - c;
+  int top[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) top[e] = tops[kBM + wn + c + e];
 #pragma unroll
   for (int i = 0; i < kTM; ++i) {
 #pragma unroll
     for (int j = 0; j < kTN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        Out* const q = slab + (lane & 31) * kPitch + 32 * j + 2 * e + 4 * (lane >> 5);
-        v4f v = {acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-        if (any) {
-          const v4i top =
-              *reinterpret_cast<const v4i*>(tops + kBM + wn + 32 * j + 2 * e + 4 * (lane >> 5));
-#pragma unroll
-          for (int c = 0; c < 4; ++c) v[c] = __builtin_ldexpf(v[c], top_a[i] + top[c]);
-        }
-        if constexpr (sizeof(Out) == 4) *reinterpret_cast<v4f*>(q) = v;
-        else *reinterpret_cast<v4b*>(q) = __builtin_convertvector(v, v4b);
-      }
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<v4f*>(slab + (lane & 31) * kPitch + 32 * j + 2 * e + 4 * (lane >> 5)) =
+            v4f{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
     __builtin_amdgcn_wave_barrier();
-    constexpr int kRun = kWN / kPer, kStep = 64 / kRun;  // lanes of a row, rows of a store
-    const int c = lane % kRun * kPer;
-    if (rows >= 32 * (i + 1) && cols >= kWN) {
-#pragma unroll
-      for (int r = 0; r < 32; r += kStep) {
-        const int rr = r + lane / kRun;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(slab + rr * kPitch + c);
-        __builtin_nontemporal_store(v, reinterpret_cast<u32x4_h*>(out + (32 * i + rr) * p.ld_out + c));
-      }
-    } else {
 #pragma unroll 1
-      for (int r = lane / kRun; r < 32 && 32 * i + r < rows; r += kStep)
-        store_units(out + (32 * i + r) * p.ld_out + c,
-                    *reinterpret_cast<const u32x4*>(slab + r * kPitch + c), cols - c);
+    for (int r = lane / kRun; r < 32; r += 64 / kRun) {
+      if (32 * i + r >= rows) break;
+      const int row_top = tops[wm + 32 * i + r];
+      float v[kPer];
+#pragma unroll
+      for (int e = 0; e < kPer; e += 4) {
+        const v4f w = *reinterpret_cast<const v4f*>(slab + r * kPitch + c + e);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[e + q] = __builtin_ldexpf(w[q], row_top + top[e + q]);
+      }
+      u32x4 u;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if constexpr (sizeof(Out) == 4) u[q] = __float_as_uint(v[q]);
+        else u[q] = pack_bf16(v[2 * q], v[2 * q + 1]);
+      }
+      Out* const o = out + (32 * i + r) * p.ld_out;
+      if (cols >= kPer) __builtin_nontemporal_store(u, reinterpret_cast<u32x4_h*>(o));
+      else store_units(o, u, cols);
     }
     __builtin_amdgcn_wave_barrier();
   }
