@@ -146,8 +146,8 @@ def matmul_fp8_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def matmul_fp8(a: Fp8, b: Fp8, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16,
                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """a @ b.T of two 8-bit operands of the same width (zf_matmul_fp8), in bf16
-    or fp32 (out's type where it is given).  A linear layer of weight w [n, k]:
+    """a @ b.T of two 8-bit operands of the same width (zf_matmul_fp8), summed in
+    fp32, in bf16 or fp32 (out's type where it is given).  A linear layer of weight w [n, k]:
     forward matmul_fp8(x, w), input gradient matmul_fp8(dy, wt), weight
     gradient matmul_fp8(dyt, xt) in ROW_MAJOR or matmul_fp8(xt, dyt) in
     CHANNEL_MAJOR, with *t the transposed copies of quantize_fp8."""
