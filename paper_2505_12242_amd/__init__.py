@@ -4,8 +4,9 @@ Per bf16 weight gradient: per-input-channel squared norms, top-k channel
 selection, in-place Adam on the selected channels' fp32 states with bf16
 write-back, and S-step accumulation of the unselected channels in a packed
 fp32 buffer handed over as a dense matrix.  Around it, the layer the weights belong
-to: RMS norm, 8-bit quantiser and matrix product, and AdamW over the many
-tensors that are not split by channel (layer.py).  All of it runs in the HIP
+to: RMS norm and layer norm, 8-bit quantiser, matrix product and linear layer,
+attention (attention.py), and AdamW over the many tensors that are not split by
+channel (layer.py).  All of it runs in the HIP
 kernels of libzf.so (C ABI in include/); this package only binds it.
 """
 
@@ -44,12 +45,29 @@ from ._lib import (  # noqa: F401
     update_fused,
     update_fused_handover,
 )
+from .attention import (  # noqa: F401
+    Attention,
+    attention,
+    attention_backward,
+    attention_backward_workspace_bytes,
+    attention_workspace_bytes,
+)
 from .layer import (  # noqa: F401
     AdamWBuffers,
     AdamWPlan,
     Fp8,
+    LayerNorm,
+    LinearFp8,
+    LinearFp8Grad,
     RmsNorm,
     alloc_fp8,
+    layernorm,
+    layernorm_backward,
+    layernorm_backward_workspace_bytes,
+    linear_fp8,
+    linear_fp8_backward,
+    linear_fp8_backward_workspace_bytes,
+    linear_fp8_workspace_bytes,
     matmul_fp8,
     matmul_fp8_workspace_bytes,
     quantize_fp8,

@@ -78,6 +78,22 @@ class ZfAdamwTensor(ctypes.Structure):
                 ("exp_avg_scale", c_vp), ("exp_avg_sq_scale", c_vp)]
 
 
+class ZfEpilogue(ctypes.Structure):
+    _fields_ = [("bias", c_vp), ("bias_dtype", c_i32), ("activation", c_i32), ("dtype", c_i32),
+                ("residual", c_vp), ("ld_residual", c_i64), ("z", c_vp), ("ld_z", c_i64),
+                ("y", c_vp), ("ld_y", c_i64), ("q", ctypes.POINTER(ZfFp8))]
+
+
+class ZfHeads(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("ld_token", c_i64), ("ld_head", c_i64)]
+
+
+class ZfAttention(ctypes.Structure):
+    _fields_ = [("tokens_q", c_i64), ("tokens_k", c_i64), ("sequences", c_i32), ("heads", c_i32),
+                ("kv_heads", c_i32), ("dim", c_i32), ("causal", c_i32), ("scale", c_flt),
+                ("seq_q", c_vp), ("seq_k", c_vp), ("len_k", c_vp)]
+
+
 # (name, restype, argtypes) of every exported entry point of include/*.h.
 SIGNATURES = [
     ("zf_status_string", ctypes.c_char_p, [ctypes.c_int]),
@@ -161,6 +177,28 @@ SIGNATURES = [
     ("zf_rmsnorm_backward", ctypes.c_int,
      [c_vp, c_i64, c_vp, c_i64, c_i32, c_i64, c_i64, c_vp, c_i32, c_vp, c_vp, c_i64, c_vp, c_i64,
       c_vp, c_vp, c_sz, c_vp]),
+    ("zf_layernorm_forward", ctypes.c_int,
+     [c_vp, c_i64, c_vp, c_i64, c_i32, c_i64, c_i64, c_vp, c_vp, c_i32, c_dbl, c_vp, c_i64, c_vp,
+      c_i64, ctypes.POINTER(ZfFp8), c_vp, c_vp, c_vp]),
+    ("zf_layernorm_backward_workspace_bytes", c_sz, [c_i64, c_i64]),
+    ("zf_layernorm_backward", ctypes.c_int,
+     [c_vp, c_i64, c_vp, c_i64, c_i32, c_i64, c_i64, c_vp, c_i32, c_vp, c_vp, c_vp, c_i64, c_vp,
+      c_i64, c_vp, c_vp, c_vp, c_sz, c_vp]),
+    ("zf_linear_fp8_workspace_bytes", c_sz, [c_i64, c_i64, c_i64, c_i32]),
+    ("zf_linear_fp8", ctypes.c_int,
+     [ctypes.POINTER(ZfFp8), ctypes.POINTER(ZfFp8), c_i64, c_i64, c_i64,
+      ctypes.POINTER(ZfEpilogue), c_vp, c_sz, c_vp]),
+    ("zf_linear_fp8_backward_workspace_bytes", c_sz, [c_i64, c_i64]),
+    ("zf_linear_fp8_backward", ctypes.c_int,
+     [c_vp, c_i64, c_vp, c_i64, c_i32, c_i64, c_i64, c_i32, c_vp, c_i64, ctypes.POINTER(ZfFp8),
+      ctypes.POINTER(ZfFp8), c_vp, c_vp, c_sz, c_vp]),
+    ("zf_attention_forward_workspace_bytes", c_sz, [ctypes.POINTER(ZfAttention)]),
+    ("zf_attention_forward", ctypes.c_int,
+     [ctypes.POINTER(ZfAttention)] + [ctypes.POINTER(ZfHeads)] * 4 + [c_vp, c_vp, c_sz, c_vp]),
+    ("zf_attention_backward_workspace_bytes", c_sz, [ctypes.POINTER(ZfAttention)]),
+    ("zf_attention_backward", ctypes.c_int,
+     [ctypes.POINTER(ZfAttention)] + [ctypes.POINTER(ZfHeads)] * 4 + [c_vp] +
+     [ctypes.POINTER(ZfHeads)] * 4 + [c_vp, c_sz, c_vp]),
     ("zf_adamw_plan_query", ctypes.c_int,
      [ctypes.POINTER(ZfAdamwTensor), c_i32, ctypes.POINTER(c_sz)]),
     ("zf_adamw_plan_create", ctypes.c_int,
@@ -272,6 +310,22 @@ def _workspace(t: Optional[torch.Tensor]) -> int:
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("workspace: must be a contiguous GPU tensor")
     return t.numel() * t.element_size()
+
+
+def _same_device(stream, **tensors) -> None:
+    """Refuses tensors of different GPUs, and of another one than the launch's."""
+    first = None
+    for name, t in tensors.items():
+        if t is None or not t.is_cuda:
+            continue
+        index = t.get_device()
+        if first is None:
+            first = index
+            on = stream.device.index if stream is not None else torch._C._cuda_getDevice()
+            if index != on:
+                raise ValueError(f"{name}: lives on GPU {index}, the call is launched on GPU {on}")
+        elif index != first:
+            raise ValueError(f"{name}: lives on GPU {index}, other arguments on GPU {first}")
 
 
 def _logical(t: torch.Tensor, layout: int):

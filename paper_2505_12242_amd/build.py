@@ -25,7 +25,8 @@ ARCH = "gfx950"
 
 SOURCES = ["zf_api.hip", "zf_kernels.hip", "zf_kernels_cm.hip", "zf_kernels_zen.hip",
            "zf_kernels_offload.hip", "zf_kernels_rv.hip", "zf_kernels_stream.hip", "zf_layer_api.hip",
-           "zf_fp8.hip", "zf_matmul.hip", "zf_norm.hip", "zf_adamw.hip", "zf_host.cpp"]
+           "zf_fp8.hip", "zf_matmul.hip", "zf_norm.hip", "zf_layernorm.hip", "zf_linear.hip",
+           "zf_attention.hip", "zf_attention_bwd.hip", "zf_adamw.hip", "zf_host.cpp"]
 
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-pthread",

@@ -1,0 +1,214 @@
+// Shared by the attention kernels (formulas in zf_layer.h).
+//
+// Rows.  The query heads of one key head are rows of the same products: row r
+// of a sequence is query token r / group, head r % group of the key head's
+// `group` query heads.  A single token of a model with 8 query heads to a key
+// head is 8 rows over one read of the cache, and the gradients of k and v sum
+// over the heads inside the products.
+//
+// Products.  32 x 32 x 16 bf16 products with fp32 sums.  A lane holds 8
+// consecutive elements of row lane % 32 of either operand, half = lane / 32
+// saying which 8 of the 16; of the result it holds column lane % 32, rows
+// 8 (r / 4) + 4 half + r % 4 in registers r = 0 .. 15.  So the result's
+// registers 8 c .. 8 c + 7, rounded to bf16, are one operand of a product that
+// sums over the rows 16 c .. 16 c + 15, taken in the order
+// 4 half + {0 .. 3}, 8 + 4 half + {0 .. 3}: scores become weights of the next
+// product where they stand.  The other operand has to come in the same order,
+// transposed: two transposing reads of LDS, 4 rows each, give it (frag_t).
+#pragma once
+
+#include "zf_layer.hpp"
+
+namespace zf {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef __bf16 v4b __attribute__((ext_vector_type(4)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Rows of 8-element units (16 bytes) in LDS, as frag and frag_t read them.
+// DP: the head's width rounded up to one of 64, 96, 128.
+template <int DP>
+struct Heads {
+  static constexpr int kPitch = DP <= 64 ? 128 : 256;  // bytes of a row
+  static constexpr int kUnits = kPitch / 16;
+  static constexpr int kChunks = DP / 16;  // of a sum over the head's width
+  static constexpr int kTiles = DP / 32;   // of a result that wide
+  static constexpr int kPer = 1024 / kPitch;  // rows that a wave loads at once
+
+  // The unit's place in row r: 16 consecutive rows reading one unit, and 4 rows
+  // reading 4 consecutive units, meet every bank once.
+  static __device__ __forceinline__ int swizzle(int r) {
+    return kUnits == 16 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+  }
+  static __device__ __forceinline__ int at(int r, int unit) {
+    return r * kPitch + ((unit ^ swizzle(r)) << 4);
+  }
+
+  // Chunk c of rows r0 .. r0 + 31 (r0 a multiple of 16), a row a lane.
+  static __device__ __forceinline__ v8b frag(const uint8_t* lds, int r0, int c) {
+    const int lane = threadIdx.x & 63;
+    return *reinterpret_cast<const v8b*>(lds + r0 * kPitch +
+                                         at(lane & 31, 2 * c + (lane >> 5)));
+  }
+  // Columns 32 t .. 32 t + 31, a column a lane, of rows r0 .. r0 + 15 (r0 a
+  // multiple of 16) in the order above.
+  static __device__ __forceinline__ v8b frag_t(uint8_t* lds, int r0, int t) {
+    const int lane = threadIdx.x & 63, i = lane & 15;
+    const int row = 4 * (lane >> 5) + (i >> 2), unit = 4 * t + (lane >> 3 & 2) + (i >> 1 & 1);
+    v4s x[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) v4s*)(lds + r0 * kPitch + at(8 * e + row, unit) +
+                                                   8 * (i & 1)));
+    return __builtin_bit_cast(
+        v8b, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// A product of 32 rows of a and of b: b's rows along the lanes of the result.
+__device__ __forceinline__ v16f mma(v8b a, v8b b, v16f c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ v16f zero16() {
+  v16f z;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+  return z;
+}
+// The result's row in register r, of the lane's half.
+__device__ __forceinline__ int reg_row(int r) { return 8 * (r >> 2) + (r & 3); }
+
+// Registers 8 c .. 8 c + 7 rounded to bf16.
+__device__ __forceinline__ v8b pack8(const v16f& s, int c) {
+  u32x4 u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = pack_bf16(s[8 * c + 2 * i], s[8 * c + 2 * i + 1]);
+  return __builtin_bit_cast(v8b, u);
+}
+
+// x of the lane with the same lane % 32 in the other half joined with the lane's.
+__device__ __forceinline__ float other_half(float x) {
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float((threadIdx.x & 32) ? t[0] : t[1]);
+}
+
+struct HeadsArg {
+  uint16_t* p;
+  int64_t ld_token, ld_head;
+};
+struct AttentionArgs {
+  HeadsArg q, k, v;
+  uint16_t* out;
+  int64_t ld_out_token, ld_out_head;
+  float* lse;
+  const int32_t* seq_q;
+  const int32_t* seq_k;
+  const int32_t* len_k;
+  int64_t tokens_q, tokens_k;
+  int32_t sequences, heads, kv_heads, group, dim, causal;
+  int32_t tiles;   // of rows, of one key head (an upper bound)
+  int32_t splits;  // of the keys
+  float scale;
+  float* part_out;  // [splits][heads][tokens_q][dim]
+  float* part_lse;  // [splits][heads][tokens_q]
+};
+
+// A sequence, and where one of its tiles (of rows, or of keys) begins.
+struct Sequence {
+  int32_t q0, lq, k0, lk;
+  int32_t rows, first;
+};
+
+__device__ __forceinline__ int32_t clamp_token(int32_t x, int64_t tokens) {
+  return x < 0 ? 0 : x > tokens ? static_cast<int32_t>(tokens) : x;
+}
+
+// Tile `g` of the tiles of 2^lg rows (KEYS: of keys): sequence s has the tiles
+// from (start * group >> lg) + s on, which are at least as many as it needs
+// before the next one's.  So no list of tiles is built, and a captured call
+// follows the lengths.  The wave searches 64 sequences at a time.  False: no
+// such tile.
+template <bool KEYS, typename Args>
+__device__ __forceinline__ bool find_tile(const Args& a, int64_t g, int lg, Sequence& w) {
+  const int64_t group = KEYS ? 1 : a.group;
+  int32_t s = 0;
+  if (a.seq_q != nullptr) {
+    const int32_t* const starts = KEYS ? a.seq_k : a.seq_q;
+    const int64_t tokens = KEYS ? a.tokens_k : a.tokens_q;
+    const int lane = threadIdx.x & 63;
+    int32_t count = a.sequences;
+    do {
+      const int32_t step = (count + 63) / 64;
+      const int64_t at = static_cast<int64_t>(lane) * step;
+      bool ok = false;
+      if (at < count) {
+        const int32_t i = s + static_cast<int32_t>(at);
+        ok = (clamp_token(starts[i], tokens) * group >> lg) + i <= g;
+      }
+      const uint64_t found = __ballot(ok);
+      if (found == 0) return false;
+      const int32_t last = 63 - __builtin_clzll(found);
+      s += last * step;
+      count = min(step, count - last * step);
+    } while (count > 1);
+    s = uniform_i32(s);
+    w.q0 = clamp_token(a.seq_q[s], a.tokens_q);
+    w.lq = max(clamp_token(a.seq_q[s + 1], a.tokens_q) - w.q0, 0);
+    w.k0 = clamp_token(a.seq_k[s], a.tokens_k);
+    w.lk = max(clamp_token(a.seq_k[s + 1], a.tokens_k) - w.k0, 0);
+    if (a.len_k != nullptr) w.lk = min(w.lk, max(a.len_k[s], 0));
+  } else {
+    w.q0 = w.k0 = 0;
+    w.lq = static_cast<int32_t>(a.tokens_q);
+    w.lk = static_cast<int32_t>(a.tokens_k);
+  }
+  w.q0 = uniform_i32(w.q0);
+  w.lq = uniform_i32(w.lq);
+  w.k0 = uniform_i32(w.k0);
+  w.lk = uniform_i32(w.lk);
+  w.rows = w.lq * a.group;
+  const int64_t first = (g - (((KEYS ? w.k0 : w.q0) * group >> lg) + s)) << lg;
+  if (first >= (KEYS ? w.lk : w.rows)) return false;
+  w.first = static_cast<int32_t>(first);
+  return true;
+}
+
+// Keys that query token i of a sequence sees.
+template <typename Args>
+__device__ __forceinline__ int32_t keys_of(const Args& a, const Sequence& w, int32_t i) {
+  return a.causal ? max(min(w.lk, i + w.lk - w.lq + 1), 0) : w.lk;
+}
+
+// 16 bytes a lane from memory to LDS, at lds + lane * 16 (`lds` the same in
+// every lane).
+__device__ __forceinline__ void dma16(rsrc_t r, uint8_t* lds, uint32_t voff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16,
+                                           voff, 0, 0, 0);
+}
+
+size_t attention_workspace(const AttentionArgs& a);
+hipError_t launch_attention(AttentionArgs a, void* ws, hipStream_t s);
+
+struct AttentionBwdArgs {
+  HeadsArg q, k, v, out, dout;
+  HeadsArg dq, dk, dv;  // (written)
+  const float* lse;
+  float* delta;  // [heads][tokens_q]
+  const int32_t* seq_q;
+  const int32_t* seq_k;
+  const int32_t* len_k;  // nullptr
+  int64_t tokens_q, tokens_k;
+  int32_t sequences, heads, kv_heads, group, dim, causal;
+  int32_t tiles, key_tiles;
+  float scale;
+};
+size_t attention_backward_workspace(const AttentionBwdArgs& a);
+hipError_t launch_attention_backward(AttentionBwdArgs a, void* ws, hipStream_t s);
+
+}  // namespace zf

@@ -1,0 +1,296 @@
+// Attention's gradients (formulas and contract in zf_layer.h; rows, products and
+// the layout of LDS in zf_attention.hpp).
+//
+// Two kernels.  The first takes 128 rows a block, as the forward pass does, and
+// walks their keys: scores again, dP, dS, dq; before that it forms d = dout . out
+// of its rows, which the second needs too.  The second takes 128 keys a block and
+// walks the rows that see them, over all query heads of the key head: scores, dP,
+// dk and dv.  Seven products in place of the five that one kernel needs, but no
+// gradient is summed across blocks: no atomics, no partial results in memory, and
+// the same bits on every run.
+//
+// In either, the operand that a wave keeps (rows, or keys) stays in registers and
+// runs along the lanes of the scores; what is walked runs along their registers,
+// so that P and dS, rounded to bf16, are operands of the second products where
+// they stand.
+#include <algorithm>
+
+#include "zf_attention.hpp"
+
+namespace zf {
+namespace {
+
+constexpr int kLg = 7, kBlock = 1 << kLg;  // rows, or keys, of a block
+constexpr int kKeys = 64;                  // keys of a tile (dq)
+constexpr int kRows = 32;                  // rows of a tile (dk, dv)
+
+// A vector as the lane's part of an operand: 8 elements of each chunk of 16,
+// zeros past the head's width.
+template <int DP>
+__device__ __forceinline__ void load_vector(const uint16_t* p, int dim, v8b (&x)[DP / 16]) {
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) {
+    const int e = 16 * c + 8 * (threadIdx.x >> 5 & 1);
+    u32x4 u = {0, 0, 0, 0};
+    if (e < dim) u = *reinterpret_cast<const u32x4*>(p + e);
+    x[c] = __builtin_bit_cast(v8b, u);
+  }
+}
+
+// A gradient's vector, along the lane's registers of a result.
+template <int DP>
+__device__ __forceinline__ void store_vector(uint16_t* p, int dim, const v16f (&x)[DP / 32],
+                                             float scale) {
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * t + 8 * g + 4 * (threadIdx.x >> 5 & 1);
+      if (d < dim)
+        *reinterpret_cast<u32x2*>(p + d) =
+            u32x2{pack_bf16(x[t][4 * g] * scale, x[t][4 * g + 1] * scale),
+                  pack_bf16(x[t][4 * g + 2] * scale, x[t][4 * g + 3] * scale)};
+    }
+}
+
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a) {
+  typedef Heads<DP> H;
+  constexpr int kTile = kKeys * H::kPitch, kLoads = kKeys / H::kPer / 4;  // loads of a wave
+  __shared__ __align__(1024) uint8_t lds[4 * kTile];  // two slots of k and v
+  const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6), half = lane >> 5;
+  const int32_t kvh = blockIdx.x % a.kv_heads;
+  Sequence w;
+  if (!find_tile<false>(a, a.tiles - 1 - static_cast<int64_t>(blockIdx.x / a.kv_heads), kLg, w))
+    return;
+  const int32_t row = w.first + 32 * wave + (lane & 31);
+  const bool valid = row < w.rows;
+  const int32_t i = min(row, w.rows - 1) / a.group;
+  const int64_t head = kvh * a.group + min(row, w.rows - 1) - i * a.group;
+  const int64_t token = w.q0 + i;
+  v8b q[H::kChunks], dout[H::kChunks];
+  load_vector<DP>(a.q.p + token * a.q.ld_token + head * a.q.ld_head, a.dim, q);
+  load_vector<DP>(a.dout.p + token * a.dout.ld_token + head * a.dout.ld_head, a.dim, dout);
+  float delta = 0.0f;
+  {
+    v8b out[H::kChunks];
+    load_vector<DP>(a.out.p + token * a.out.ld_token + head * a.out.ld_head, a.dim, out);
+#pragma unroll
+    for (int c = 0; c < H::kChunks; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        delta = fmaf(static_cast<float>(dout[c][e]), static_cast<float>(out[c][e]), delta);
+    delta += other_half(delta);
+  }
+  if (valid && lane < 32) a.delta[head * a.tokens_q + token] = delta;
+  const float lse = a.lse[head * a.tokens_q + token] * kLog2E, c = a.scale * kLog2E;
+  const int32_t lim = keys_of(a, w, i);
+  v16f acc[H::kTiles];
+#pragma unroll
+  for (int t = 0; t < H::kTiles; ++t) acc[t] = zero16();
+
+  const auto token_of = [&](int32_t row) { return min(row, w.rows - 1) / a.group; };
+  const int32_t least = uniform_i32(keys_of(a, w, token_of(w.first + 32 * wave)));
+  const int32_t most =
+      uniform_i32(w.first + 32 * wave < w.rows ? keys_of(a, w, token_of(w.first + 32 * wave + 31)) : 0);
+  const int32_t end = uniform_i32(keys_of(a, w, token_of(w.first + kBlock - 1)));
+  const uint32_t ldk = static_cast<uint32_t>(a.k.ld_token) * 2, ldv = static_cast<uint32_t>(a.v.ld_token) * 2;
+  const uint16_t* const kp = a.k.p + kvh * a.k.ld_head;
+  const uint16_t* const vp = a.v.p + kvh * a.v.ld_head;
+  const auto load = [&](int32_t kb, int slot) {
+    const int64_t t0 = static_cast<int64_t>(w.k0) + kb;
+    const rsrc_t rk = make_rsrc(kp + t0 * a.k.ld_token, -1), rv = make_rsrc(vp + t0 * a.v.ld_token, -1);
+    const int last = w.lk - 1 - kb;
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int r = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
+      const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
+      const uint32_t row = static_cast<uint32_t>(min(r, last));
+      uint8_t* const p = lds + slot * 2 * kTile + (wave * kLoads + n) * 1024;
+      dma16(rk, p, row * ldk + unit * 16);
+      dma16(rv, p + kTile, row * ldv + unit * 16);
+    }
+  };
+  if (end > 0) load(0, 0);
+  int slot = 0;
+  for (int32_t kb = 0; kb < end; kb += kKeys) {
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (kb + kKeys < end) load(kb + kKeys, slot ^ 1);
+    uint8_t* const k = lds + slot * 2 * kTile;
+    const uint8_t* const v = k + kTile;
+    if (kb < most) {
+      const bool mask = kb + kKeys > least;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        v16f s = zero16(), dp = zero16();
+#pragma unroll
+        for (int j = 0; j < H::kChunks; ++j) s = mma(H::frag(k, 32 * t, j), q[j], s);
+#pragma unroll
+        for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(v, 32 * t, j), dout[j], dp);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse)) * (dp[r] - delta);
+        if (mask) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (kb + 32 * t + reg_row(r) + 4 * half >= lim) s[r] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const v8b ds = pack8(s, j);
+#pragma unroll
+          for (int u = 0; u < H::kTiles; ++u)
+            acc[u] = mma(H::frag_t(k, 32 * t + 16 * j, u), ds, acc[u]);
+        }
+      }
+    }
+    slot ^= 1;
+  }
+  if (valid)
+    store_vector<DP>(a.dq.p + token * a.dq.ld_token + head * a.dq.ld_head, a.dim, acc, a.scale);
+}
+
+template <int DP>
+__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionBwdArgs a) {
+  typedef Heads<DP> H;
+  constexpr int kTile = kRows * H::kPitch, kLoads = kRows / H::kPer / 4;
+  constexpr int kSlot = 2 * kTile + 512;              // q, dout, lse and delta of the rows
+  __shared__ __align__(1024) uint8_t lds[2 * kSlot];
+  const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6), half = lane >> 5;
+  const int32_t kvh = blockIdx.x % a.kv_heads;
+  Sequence w;
+  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, kLg, w)) return;
+  const int32_t key = w.first + 32 * wave + (lane & 31);
+  const bool valid = key < w.lk;
+  const int64_t token = w.k0 + min(key, w.lk - 1);
+  v8b k[H::kChunks], v[H::kChunks];
+  load_vector<DP>(a.k.p + token * a.k.ld_token + kvh * a.k.ld_head, a.dim, k);
+  load_vector<DP>(a.v.p + token * a.v.ld_token + kvh * a.v.ld_head, a.dim, v);
+  v16f dk[H::kTiles], dv[H::kTiles];
+#pragma unroll
+  for (int t = 0; t < H::kTiles; ++t) dk[t] = dv[t] = zero16();
+  // the first row that sees a key (of any query head)
+  const auto first_row = [&](int32_t key) {
+    return a.causal ? max(key - (w.lk - w.lq), 0) * a.group : 0;
+  };
+  const int32_t from = first_row(min(key, w.lk - 1));
+  const int32_t most = uniform_i32(first_row(min(w.first + 32 * wave + 31, w.lk - 1)));
+  const int32_t least = uniform_i32(
+      w.first + 32 * wave < w.lk ? first_row(w.first + 32 * wave) : w.rows);
+  const int32_t begin = uniform_i32(first_row(w.first)) / kRows * kRows;
+
+  const uint32_t ldq = static_cast<uint32_t>(a.q.ld_token) * 2, ldo = static_cast<uint32_t>(a.dout.ld_token) * 2;
+  const uint32_t lhq = static_cast<uint32_t>(a.q.ld_head) * 2, lho = static_cast<uint32_t>(a.dout.ld_head) * 2;
+  const int64_t head0 = static_cast<int64_t>(kvh) * a.group;
+  const rsrc_t rl = make_rsrc(a.lse + head0 * a.tokens_q + w.q0, -1);
+  const rsrc_t rd = make_rsrc(a.delta + head0 * a.tokens_q + w.q0, -1);
+  const uint32_t magic = 0xffffffffu / static_cast<uint32_t>(a.group) + 1;  // (0: a group of one)
+  const auto load = [&](int32_t r0, int slot) {
+    const int32_t t0 = uniform_i32(r0 / a.group);
+    const uint32_t in = static_cast<uint32_t>(r0 - t0 * a.group);
+    const int64_t tok = static_cast<int64_t>(w.q0) + t0;
+    const rsrc_t rq = make_rsrc(a.q.p + tok * a.q.ld_token + head0 * a.q.ld_head, -1);
+    const rsrc_t ro = make_rsrc(a.dout.p + tok * a.dout.ld_token + head0 * a.dout.ld_head, -1);
+    const int last = w.rows - 1 - r0;
+    const auto split = [&](int r, uint32_t& tok, uint32_t& g) {  // row r0 + r
+      const uint32_t x = in + static_cast<uint32_t>(min(r, last));
+      tok = magic ? __umulhi(x, magic) : x;
+      g = x - tok * static_cast<uint32_t>(a.group);
+    };
+    uint32_t tk, g;
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int r = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
+      const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
+      split(r, tk, g);
+      uint8_t* const p = lds + slot * kSlot + (wave * kLoads + n) * 1024;
+      dma16(rq, p, tk * ldq + g * lhq + unit * 16);
+      dma16(ro, p + kTile, tk * ldo + g * lho + unit * 16);
+    }
+    if (wave < 2) {  // (lanes 32 and up repeat the rows, behind them)
+      split(lane & 31, tk, g);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          wave == 0 ? rl : rd,
+          (__attribute__((address_space(3))) void*)(lds + slot * kSlot + 2 * kTile + wave * 256), 4,
+          (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4, 0, 0, 0);
+    }
+  };
+  const float c = a.scale * kLog2E;
+  if (begin < w.rows) load(begin, 0);
+  int slot = 0;
+  for (int32_t r0 = begin; r0 < w.rows; r0 += kRows) {
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (r0 + kRows < w.rows) load(r0 + kRows, slot ^ 1);
+    uint8_t* const q = lds + slot * kSlot;
+    uint8_t* const dout = q + kTile;
+    const float* const stats = reinterpret_cast<const float*>(q + 2 * kTile);
+    if (r0 + kRows > least) {
+      v16f s = zero16(), dp = zero16();
+#pragma unroll
+      for (int j = 0; j < H::kChunks; ++j) s = mma(H::frag(q, 0, j), k[j], s);
+#pragma unroll
+      for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(dout, 0, j), v[j], dp);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int at = 8 * g + 4 * half;
+        const u32x4 l = *reinterpret_cast<const u32x4*>(stats + at);
+        const u32x4 d = *reinterpret_cast<const u32x4*>(stats + 64 + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -(__uint_as_float(l[e]) * kLog2E)));
+          dp[r] = s[r] * (dp[r] - __uint_as_float(d[e]));
+        }
+      }
+      if (r0 < most || r0 + kRows > w.rows) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int32_t row = r0 + reg_row(r) + 4 * half;
+          if (row < from || row >= w.rows) s[r] = dp[r] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const v8b p = pack8(s, j), ds = pack8(dp, j);
+#pragma unroll
+        for (int t = 0; t < H::kTiles; ++t) dv[t] = mma(H::frag_t(dout, 16 * j, t), p, dv[t]);
+#pragma unroll
+        for (int t = 0; t < H::kTiles; ++t) dk[t] = mma(H::frag_t(q, 16 * j, t), ds, dk[t]);
+      }
+    }
+    slot ^= 1;
+  }
+  if (valid) {
+    store_vector<DP>(a.dk.p + token * a.dk.ld_token + kvh * a.dk.ld_head, a.dim, dk, a.scale);
+    store_vector<DP>(a.dv.p + token * a.dv.ld_token + kvh * a.dv.ld_head, a.dim, dv, 1.0f);
+  }
+}
+
+template <int DP>
+void launch(const AttentionBwdArgs& a, hipStream_t s) {
+  if (a.tokens_q > 0)
+    hipLaunchKernelGGL((attention_dq_kernel<DP>), dim3(static_cast<uint32_t>(a.tiles) * a.kv_heads),
+                       dim3(256), 0, s, a);
+  if (a.tokens_k > 0)
+    hipLaunchKernelGGL((attention_dkv_kernel<DP>),
+                       dim3(static_cast<uint32_t>(a.key_tiles) * a.kv_heads), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+size_t attention_backward_workspace(const AttentionBwdArgs& a) {
+  return static_cast<size_t>(a.heads) * a.tokens_q * sizeof(float);
+}
+
+hipError_t launch_attention_backward(AttentionBwdArgs a, void* ws, hipStream_t s) {
+  (void)hipGetLastError();
+  a.delta = static_cast<float*>(ws);
+  a.tiles = static_cast<int32_t>((a.tokens_q * a.group >> kLg) + a.sequences);
+  a.key_tiles = static_cast<int32_t>((a.tokens_k >> kLg) + a.sequences);
+  if (a.dim <= 64) launch<64>(a, s);
+  else if (a.dim <= 96) launch<96>(a, s);
+  else launch<128>(a, s);
+  return hipGetLastError();
+}
+
+}  // namespace zf

@@ -81,6 +81,79 @@ struct NormBwdArgs {
 size_t rmsnorm_backward_workspace(int64_t rows, int64_t cols);
 hipError_t launch_rmsnorm_backward(const NormBwdArgs& a, int32_t dtype, hipStream_t s);
 
+struct LayerNormArgs {
+  const void* x;
+  int64_t ld_x;
+  const void* residual;
+  int64_t ld_residual;
+  int64_t rows, cols;
+  const void* gain;
+  const void* bias;
+  int32_t gain_f32;
+  float eps;
+  void* h;
+  int64_t ld_h;
+  void* y;
+  int64_t ld_y;
+  Fp8Out q;
+  float* mean;
+  float* rstd;
+};
+hipError_t launch_layernorm(const LayerNormArgs& a, int32_t dtype, hipStream_t s);
+
+struct LayerNormBwdArgs {
+  const void* dy;
+  int64_t ld_dy;
+  const void* h;
+  int64_t ld_h;
+  int64_t rows, cols;
+  const void* gain;
+  int32_t gain_f32;
+  const float* mean;
+  const float* rstd;
+  const void* dres;
+  int64_t ld_dres;
+  void* dx;
+  int64_t ld_dx;
+  float* dgain;
+  float* dbias;
+  float* part;
+};
+size_t layernorm_backward_workspace(int64_t rows, int64_t cols);
+hipError_t launch_layernorm_backward(const LayerNormBwdArgs& a, int32_t dtype, hipStream_t s);
+
+struct Epilogue {
+  const void* bias;
+  int32_t bias_f32;
+  int32_t activation;
+  const void* residual;
+  int64_t ld_residual;
+  void* z;
+  int64_t ld_z;
+  void* y;
+  int64_t ld_y;
+  Fp8Out q;
+};
+size_t linear_workspace(int64_t m, int64_t n, int64_t k, bool q);
+hipError_t launch_linear(const MatmulArgs& a, const Epilogue& e, int32_t dtype, void* ws,
+                         hipStream_t s);
+
+struct LinearBwdArgs {
+  const void* dy;
+  int64_t ld_dy;
+  const void* z;
+  int64_t ld_z;
+  int64_t rows, cols;
+  int32_t activation;
+  void* dz;
+  int64_t ld_dz;
+  Fp8Out q, qt;
+  float* dbias;
+  float* part;
+};
+size_t linear_backward_workspace(int64_t rows, int64_t cols);
+hipError_t launch_linear_backward(const LinearBwdArgs& a, int32_t dtype, hipStream_t s);
+
 // AdamW: one tensor of a plan's device table.
 struct AdamTensor {
   int64_t n;

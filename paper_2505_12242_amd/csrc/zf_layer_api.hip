@@ -6,6 +6,7 @@
 #include <new>
 #include <vector>
 
+#include "zf_attention.hpp"
 #include "zf_layer.hpp"
 
 namespace {
@@ -86,6 +87,146 @@ zf::MatmulOperand operand(const zf_fp8* f) {
 }
 
 zf_status done(hipError_t e) { return e == hipSuccess ? ZF_OK : hip_fail(e); }
+
+// An output in place of an input: the same elements, or apart from it.
+bool apart_or_same(const Span& so, const void* out, int64_t ld_out, const Span& si, const void* in,
+                   int64_t ld_in, int64_t rows) {
+  return !overlaps(so, si) || (out == in && (rows <= 1 || ld_out == ld_in));
+}
+
+// A workspace of `need` bytes, 16-byte aligned, as a span.
+zf_status workspace_span(void* ws, size_t ws_bytes, size_t need, bool ok, Span& s) {
+  if (!ok) return ZF_EINVAL;
+  if (need == 0) return ZF_OK;
+  if (ws_bytes < need) return ZF_EWORKSPACE;
+  if (ws == nullptr || !aligned(ws, 16)) return ZF_EINVAL;
+  s.lo = reinterpret_cast<uintptr_t>(ws);
+  s.hi = s.lo + need;
+  return ZF_OK;
+}
+
+bool activation_ok(int32_t a) { return a >= ZF_NONE && a <= ZF_SILU; }
+
+// What a product's tiles can address (32-bit offsets inside one) and a launch hold.
+bool product_ok(const zf_fp8* a, const zf_fp8* b, int64_t m, int64_t n, int64_t k) {
+  return k < kStrideLimit &&
+         (m <= 1 || k == 0 || (a->ld_data < kStrideLimit && a->ld_scale < kStrideLimit)) &&
+         (n <= 1 || k == 0 || (b->ld_data < kStrideLimit && b->ld_scale < kStrideLimit)) &&
+         ceil_div(m, 128) * ceil_div(n, 128) < kGridLimit;
+}
+
+// ---- attention ----
+
+bool attention_ok(const zf_attention* a) {
+  if (a == nullptr || !size_ok(a->tokens_q) || !size_ok(a->tokens_k) || a->sequences < 1 ||
+      a->kv_heads < 1 || a->heads < 1 || a->heads > (1 << 16) || a->heads % a->kv_heads != 0 ||
+      a->dim < 8 || a->dim > 128 || a->dim % 8 != 0 || !std::isfinite(a->scale) || !(a->scale > 0.0f))
+    return false;
+  if ((a->seq_q == nullptr) != (a->seq_k == nullptr)) return false;
+  if (a->seq_q == nullptr && (a->sequences != 1 || a->len_k != nullptr)) return false;
+  if (!aligned(a->seq_q, 4) || !aligned(a->seq_k, 4) || !aligned(a->len_k, 4)) return false;
+  // rows and keys, of all heads, that a launch's blocks of 16 still reach (and
+  // that 32 bits count)
+  return (std::max(a->tokens_q * a->heads, a->tokens_k * a->kv_heads) / 16 +
+          static_cast<int64_t>(a->sequences) * a->kv_heads) < kGridLimit;
+}
+
+// Bytes from the first to past the last element.  `ok` is cleared where the
+// tensor is missing, misaligned or its strides outside their limits.
+Span heads_span(const zf_heads* t, int64_t tokens, int64_t heads, int64_t dim, bool& ok) {
+  Span s;
+  if (t == nullptr) ok = false;
+  if (!ok || tokens == 0) return s;
+  if (t->data == nullptr || !aligned(t->data, 16) || t->ld_token < 0 || t->ld_head < 0 ||
+      t->ld_token % 8 != 0 || t->ld_head % 8 != 0 || t->ld_token >= kStrideLimit ||
+      t->ld_head >= (int64_t(1) << 40)) {
+    ok = false;
+    return s;
+  }
+  s.lo = reinterpret_cast<uintptr_t>(t->data);
+  s.hi = s.lo + static_cast<uintptr_t>((tokens - 1) * t->ld_token + (heads - 1) * t->ld_head + dim) * 2;
+  return s;
+}
+
+// No two vectors of a tensor share an element: tokens and heads are nested one
+// way or the other.
+bool rows_apart(const zf_heads* t, int64_t tokens, int64_t heads, int64_t dim) {
+  if (tokens <= 1 && heads <= 1) return true;
+  const int64_t lt = t->ld_token, lh = t->ld_head;
+  if (tokens <= 1) return lh >= dim;
+  if (heads <= 1) return lt >= dim;
+  return (lh >= dim && lt >= (heads - 1) * lh + dim) || (lt >= dim && lh >= (tokens - 1) * lt + dim);
+}
+
+// Two tensors share no element: their bytes lie apart, or both are columns of
+// rows of one length.
+bool heads_apart(const zf_heads* a, int64_t tokens_a, int64_t heads_a, const zf_heads* b,
+                 int64_t tokens_b, int64_t heads_b, int64_t dim) {
+  bool ok = true;
+  const Span sa = heads_span(a, tokens_a, heads_a, dim, ok);
+  const Span sb = heads_span(b, tokens_b, heads_b, dim, ok);
+  if (!overlaps(sa, sb)) return true;
+  const uintptr_t row = static_cast<uintptr_t>(a->ld_token) * 2;
+  if (a->ld_token != b->ld_token || row == 0) return false;
+  const uintptr_t wa = static_cast<uintptr_t>((heads_a - 1) * a->ld_head + dim) * 2;
+  const uintptr_t wb = static_cast<uintptr_t>((heads_b - 1) * b->ld_head + dim) * 2;
+  // b's first column among a's rows
+  const uintptr_t at = sb.lo >= sa.lo ? (sb.lo - sa.lo) % row : (row - (sa.lo - sb.lo) % row) % row;
+  return at >= wa && at + wb <= row;
+}
+
+struct SequenceSpans {
+  Span q, k, len;
+};
+SequenceSpans sequence_spans(const zf_attention& a) {
+  const auto ints = [](const int32_t* p, int64_t n) {
+    Span s;
+    if (p != nullptr) {
+      s.lo = reinterpret_cast<uintptr_t>(p);
+      s.hi = s.lo + static_cast<uintptr_t>(n) * 4;
+    }
+    return s;
+  };
+  return {ints(a.seq_q, a.sequences + int64_t(1)), ints(a.seq_k, a.sequences + int64_t(1)),
+          ints(a.len_k, a.sequences)};
+}
+
+zf::HeadsArg heads_arg(const zf_heads* t) {
+  return zf::HeadsArg{static_cast<uint16_t*>(t->data), t->ld_token, t->ld_head};
+}
+
+zf::AttentionArgs attention_args(const zf_attention& a) {
+  zf::AttentionArgs r{};
+  r.seq_q = a.seq_q;
+  r.seq_k = a.seq_k;
+  r.len_k = a.len_k;
+  r.tokens_q = a.tokens_q;
+  r.tokens_k = a.tokens_k;
+  r.sequences = a.sequences;
+  r.heads = a.heads;
+  r.kv_heads = a.kv_heads;
+  r.group = a.heads / a.kv_heads;
+  r.dim = a.dim;
+  r.causal = a.causal != 0;
+  r.scale = a.scale;
+  return r;
+}
+
+zf::AttentionBwdArgs attention_bwd_args(const zf_attention& a) {
+  zf::AttentionBwdArgs r{};
+  r.seq_q = a.seq_q;
+  r.seq_k = a.seq_k;
+  r.tokens_q = a.tokens_q;
+  r.tokens_k = a.tokens_k;
+  r.sequences = a.sequences;
+  r.heads = a.heads;
+  r.kv_heads = a.kv_heads;
+  r.group = a.heads / a.kv_heads;
+  r.dim = a.dim;
+  r.causal = a.causal != 0;
+  r.scale = a.scale;
+  return r;
+}
 
 }  // namespace
 
@@ -225,6 +366,262 @@ zf_status zf_rmsnorm_backward(const void* dy, int64_t ld_dy, const void* h, int6
   const zf::NormBwdArgs a{dy, ld_dy, h, ld_h, rows, cols, gain, gain_dtype == ZF_F32, rstd,
                           dresidual, ld_dresidual, dx, ld_dx, dgain, static_cast<float*>(ws)};
   return done(zf::launch_rmsnorm_backward(a, dtype, as_stream(stream)));
+}
+
+zf_status zf_layernorm_forward(const void* x, int64_t ld_x, const void* residual,
+                               int64_t ld_residual, int32_t dtype, int64_t rows, int64_t cols,
+                               const void* gain, const void* bias, int32_t gain_dtype, double eps,
+                               void* h, int64_t ld_h, void* y, int64_t ld_y, const zf_fp8* q,
+                               float* mean, float* rstd, zf_stream stream) {
+  if (!dtype_ok(dtype) || !dtype_ok(gain_dtype) || !size_ok(rows) || !size_ok(cols) ||
+      !std::isfinite(eps) || !(eps >= 0.0))
+    return ZF_EINVAL;
+  const size_t e = dtype_size(dtype);
+  bool ok = true;
+  Span sr, sh, sy, sb;
+  Fp8Spans sq;
+  const Span sx = span(x, rows, cols, ld_x, e, ok);
+  const Span sg = span(gain, rows == 0 ? 0 : 1, cols, cols, dtype_size(gain_dtype), ok);
+  if (bias != nullptr) sb = span(bias, rows == 0 ? 0 : 1, cols, cols, dtype_size(gain_dtype), ok);
+  const Span sm = span(mean, 1, rows, rows, 4, ok);
+  const Span st = span(rstd, 1, rows, rows, 4, ok);
+  if (residual != nullptr) {
+    sr = span(residual, rows, cols, ld_residual, e, ok);
+    if (h == nullptr && rows > 0 && cols > 0) ok = false;
+  }
+  if (h != nullptr) sh = span(h, rows, cols, ld_h, e, ok);
+  if (y != nullptr) sy = span(y, rows, cols, ld_y, e, ok);
+  if (q != nullptr) {
+    if (q->group != 1) ok = false;
+    sq = fp8_spans(q, rows, cols, ok);
+  }
+  if (!ok || !disjoint({sh, sy, sq.data, sq.scale, sm, st}, {sg, sb}) ||
+      !disjoint({sy, sq.data, sq.scale, sm, st}, {sx, sr}))
+    return ZF_EINVAL;
+  // h in place of an input: the same elements, or apart from it
+  if (!apart_or_same(sh, h, ld_h, sx, x, ld_x, rows) ||
+      !apart_or_same(sh, h, ld_h, sr, residual, ld_residual, rows))
+    return ZF_EINVAL;
+  if (rows == 0) return ZF_OK;
+  const zf::LayerNormArgs a{x, ld_x, residual, ld_residual, rows, cols, gain, bias,
+                            gain_dtype == ZF_F32, static_cast<float>(eps), h, ld_h, y, ld_y,
+                            fp8_out(q), mean, rstd};
+  return done(zf::launch_layernorm(a, dtype, as_stream(stream)));
+}
+
+size_t zf_layernorm_backward_workspace_bytes(int64_t rows, int64_t cols) {
+  if (!size_ok(rows) || !size_ok(cols)) return 0;
+  return zf::layernorm_backward_workspace(rows, cols);
+}
+
+zf_status zf_layernorm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h,
+                                int32_t dtype, int64_t rows, int64_t cols, const void* gain,
+                                int32_t gain_dtype, const float* mean, const float* rstd,
+                                const void* dresidual, int64_t ld_dresidual, void* dx,
+                                int64_t ld_dx, float* dgain, float* dbias, void* ws,
+                                size_t ws_bytes, zf_stream stream) {
+  if (!dtype_ok(dtype) || !dtype_ok(gain_dtype) || !size_ok(rows) || !size_ok(cols))
+    return ZF_EINVAL;
+  const size_t e = dtype_size(dtype);
+  bool ok = true;
+  Span sr, sd, sb, sw;
+  const Span sy = span(dy, rows, cols, ld_dy, e, ok);
+  const Span sh = span(h, rows, cols, ld_h, e, ok);
+  const Span sx = span(dx, rows, cols, ld_dx, e, ok);
+  const Span sg = span(gain, rows == 0 ? 0 : 1, cols, cols, dtype_size(gain_dtype), ok);
+  const Span sm = span(mean, cols == 0 ? 0 : 1, rows, rows, 4, ok);
+  const Span st = span(rstd, cols == 0 ? 0 : 1, rows, rows, 4, ok);
+  if (dresidual != nullptr) sr = span(dresidual, rows, cols, ld_dresidual, e, ok);
+  if (dgain != nullptr) sd = span(dgain, 1, cols, cols, 4, ok);
+  if (dbias != nullptr) sb = span(dbias, 1, cols, cols, 4, ok);
+  if (dgain != nullptr || dbias != nullptr) {
+    const zf_status st_ws = workspace_span(ws, ws_bytes,
+                                           zf_layernorm_backward_workspace_bytes(rows, cols), ok, sw);
+    if (st_ws != ZF_OK) return st_ws;
+  }
+  if (!ok || !disjoint({sx, sd, sb, sw}, {sh, sg, sm, st}) || !disjoint({sd, sb, sw}, {sy, sr}))
+    return ZF_EINVAL;
+  if (!apart_or_same(sx, dx, ld_dx, sy, dy, ld_dy, rows) ||
+      !apart_or_same(sx, dx, ld_dx, sr, dresidual, ld_dresidual, rows))
+    return ZF_EINVAL;
+  if (cols == 0 || (rows == 0 && dgain == nullptr && dbias == nullptr)) return ZF_OK;
+  const zf::LayerNormBwdArgs a{dy, ld_dy, h, ld_h, rows, cols, gain, gain_dtype == ZF_F32, mean, rstd,
+                               dresidual, ld_dresidual, dx, ld_dx, dgain, dbias,
+                               static_cast<float*>(ws)};
+  return done(zf::launch_layernorm_backward(a, dtype, as_stream(stream)));
+}
+
+size_t zf_linear_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k, int32_t q) {
+  if (!size_ok(m) || !size_ok(n) || !size_ok(k) || m == 0 || n == 0) return 0;
+  return zf::linear_workspace(m, n, k, q != 0);
+}
+
+zf_status zf_linear_fp8(const zf_fp8* a, const zf_fp8* b, int64_t m, int64_t n, int64_t k,
+                        const zf_epilogue* e, void* ws, size_t ws_bytes, zf_stream stream) {
+  if (a == nullptr || b == nullptr || e == nullptr || !dtype_ok(e->dtype) ||
+      !dtype_ok(e->bias_dtype) || !activation_ok(e->activation) || !size_ok(m) || !size_ok(n) ||
+      !size_ok(k) || (e->z == nullptr && e->y == nullptr && e->q == nullptr))
+    return ZF_EINVAL;
+  bool ok = true;
+  const size_t size = dtype_size(e->dtype);
+  const Fp8Spans sa = fp8_spans(a, m, k, ok), sb = fp8_spans(b, n, k, ok);
+  Span si, sr, sz, sy, sw;
+  Fp8Spans sq;
+  if (e->bias != nullptr) si = span(e->bias, m == 0 ? 0 : 1, n, n, dtype_size(e->bias_dtype), ok);
+  if (e->residual != nullptr) sr = span(e->residual, m, n, e->ld_residual, size, ok);
+  if (e->z != nullptr) sz = span(e->z, m, n, e->ld_z, size, ok);
+  if (e->y != nullptr) sy = span(e->y, m, n, e->ld_y, size, ok);
+  if (e->q != nullptr) {
+    if (e->q->group != 1) ok = false;
+    sq = fp8_spans(e->q, m, n, ok);
+  }
+  if (!product_ok(a, b, m, n, k)) ok = false;
+  if (!ok) return ZF_EINVAL;
+  const zf_status st_ws =
+      workspace_span(ws, ws_bytes, zf_linear_fp8_workspace_bytes(m, n, k, e->q != nullptr), ok, sw);
+  if (st_ws != ZF_OK) return st_ws;
+  if (!disjoint({sz, sy, sq.data, sq.scale, sw},
+                {sa.data, sa.scale, sb.data, sb.scale, si}) ||
+      !disjoint({sz, sq.data, sq.scale, sw}, {sr}) ||
+      !apart_or_same(sy, e->y, e->ld_y, sr, e->residual, e->ld_residual, m))
+    return ZF_EINVAL;
+  if (m == 0 || n == 0) return ZF_OK;
+  const zf::MatmulArgs args{operand(a), operand(b), m, n, k, nullptr, 0, 0, 0};
+  const zf::Epilogue ep{e->bias, e->bias_dtype == ZF_F32, e->activation, e->residual, e->ld_residual,
+                        e->z, e->ld_z, e->y, e->ld_y, fp8_out(e->q)};
+  return done(zf::launch_linear(args, ep, e->dtype, ws, as_stream(stream)));
+}
+
+size_t zf_linear_fp8_backward_workspace_bytes(int64_t rows, int64_t cols) {
+  if (!size_ok(rows) || !size_ok(cols)) return 0;
+  return zf::linear_backward_workspace(rows, cols);
+}
+
+zf_status zf_linear_fp8_backward(const void* dy, int64_t ld_dy, const void* z, int64_t ld_z,
+                                 int32_t dtype, int64_t rows, int64_t cols, int32_t activation,
+                                 void* dz, int64_t ld_dz, const zf_fp8* q, const zf_fp8* q_t,
+                                 float* dbias, void* ws, size_t ws_bytes, zf_stream stream) {
+  if (!dtype_ok(dtype) || !size_ok(rows) || !size_ok(cols) || !activation_ok(activation) ||
+      (dz == nullptr && q == nullptr && q_t == nullptr && dbias == nullptr))
+    return ZF_EINVAL;
+  const size_t e = dtype_size(dtype);
+  bool ok = true;
+  Span sz, sd, sb, sw;
+  Fp8Spans sq, st;
+  const Span sy = span(dy, rows, cols, ld_dy, e, ok);
+  if (activation != ZF_NONE) sz = span(z, rows, cols, ld_z, e, ok);
+  if (dz != nullptr) sd = span(dz, rows, cols, ld_dz, e, ok);
+  if (q != nullptr) {
+    if (q->group != 1) ok = false;
+    sq = fp8_spans(q, rows, cols, ok);
+  }
+  if (q_t != nullptr) {
+    if (q_t->group != 1) ok = false;
+    st = fp8_spans(q_t, cols, rows, ok);
+  }
+  if (dbias != nullptr) {
+    sb = span(dbias, 1, cols, cols, 4, ok);
+    const zf_status st_ws = workspace_span(
+        ws, ws_bytes, zf_linear_fp8_backward_workspace_bytes(rows, cols), ok, sw);
+    if (st_ws != ZF_OK) return st_ws;
+  }
+  if (!ok || ceil_div(rows, 128) * ceil_div(cols, 128) >= kGridLimit ||
+      !disjoint({sd, sq.data, sq.scale, st.data, st.scale, sb, sw}, {}) ||
+      !disjoint({sq.data, sq.scale, st.data, st.scale, sb, sw}, {sy, sz}) ||
+      !apart_or_same(sd, dz, ld_dz, sy, dy, ld_dy, rows) ||
+      !apart_or_same(sd, dz, ld_dz, sz, z, ld_z, rows))
+    return ZF_EINVAL;
+  if (cols == 0 || (rows == 0 && dbias == nullptr)) return ZF_OK;
+  const zf::LinearBwdArgs a{dy, ld_dy, z, ld_z, rows, cols, activation, dz, ld_dz, fp8_out(q),
+                            fp8_out(q_t), dbias, static_cast<float*>(ws)};
+  return done(zf::launch_linear_backward(a, dtype, as_stream(stream)));
+}
+
+// ---- attention ---------------------------------------------------------------
+
+size_t zf_attention_forward_workspace_bytes(const zf_attention* a) {
+  if (!attention_ok(a)) return 0;
+  return zf::attention_workspace(attention_args(*a));
+}
+
+zf_status zf_attention_forward(const zf_attention* a, const zf_heads* q, const zf_heads* k,
+                               const zf_heads* v, const zf_heads* out, float* lse, void* ws,
+                               size_t ws_bytes, zf_stream stream) {
+  if (!attention_ok(a)) return ZF_EINVAL;
+  bool ok = true;
+  const Span sq = heads_span(q, a->tokens_q, a->heads, a->dim, ok);
+  const Span sk = heads_span(k, a->tokens_k, a->kv_heads, a->dim, ok);
+  const Span sv = heads_span(v, a->tokens_k, a->kv_heads, a->dim, ok);
+  const Span so = heads_span(out, a->tokens_q, a->heads, a->dim, ok);
+  if (!ok || !rows_apart(out, a->tokens_q, a->heads, a->dim)) return ZF_EINVAL;
+  Span sl, sw;
+  if (lse != nullptr) sl = span(lse, a->heads, a->tokens_q, a->tokens_q, 4, ok);
+  const SequenceSpans ss = sequence_spans(*a);
+  const zf_status st_ws =
+      workspace_span(ws, ws_bytes, zf_attention_forward_workspace_bytes(a), ok, sw);
+  if (st_ws != ZF_OK) return st_ws;
+  if (!disjoint({so, sl, sw}, {sq, sk, sv, ss.q, ss.k, ss.len})) return ZF_EINVAL;
+  if (a->tokens_q == 0) return ZF_OK;
+  zf::AttentionArgs args = attention_args(*a);
+  args.q = heads_arg(q);
+  args.k = heads_arg(k);
+  args.v = heads_arg(v);
+  args.out = static_cast<uint16_t*>(out->data);
+  args.ld_out_token = out->ld_token;
+  args.ld_out_head = out->ld_head;
+  args.lse = lse;
+  return done(zf::launch_attention(args, ws, as_stream(stream)));
+}
+
+size_t zf_attention_backward_workspace_bytes(const zf_attention* a) {
+  if (!attention_ok(a) || a->len_k != nullptr) return 0;
+  return zf::attention_backward_workspace(attention_bwd_args(*a));
+}
+
+zf_status zf_attention_backward(const zf_attention* a, const zf_heads* q, const zf_heads* k,
+                                const zf_heads* v, const zf_heads* out, const float* lse,
+                                const zf_heads* dout, const zf_heads* dq, const zf_heads* dk,
+                                const zf_heads* dv, void* ws, size_t ws_bytes, zf_stream stream) {
+  if (!attention_ok(a) || a->len_k != nullptr) return ZF_EINVAL;
+  const int64_t tq = a->tokens_q, tk = a->tokens_k;
+  const int32_t h = a->heads, kv = a->kv_heads, d = a->dim;
+  bool ok = true;
+  const Span sq = heads_span(q, tq, h, d, ok), sk = heads_span(k, tk, kv, d, ok),
+             sv = heads_span(v, tk, kv, d, ok), so = heads_span(out, tq, h, d, ok),
+             sdo = heads_span(dout, tq, h, d, ok), sdq = heads_span(dq, tq, h, d, ok),
+             sdk = heads_span(dk, tk, kv, d, ok), sdv = heads_span(dv, tk, kv, d, ok);
+  if (!ok || !rows_apart(dq, tq, h, d) || !rows_apart(dk, tk, kv, d) || !rows_apart(dv, tk, kv, d))
+    return ZF_EINVAL;
+  // (a tile's rows are addressed through 32-bit offsets, over a key head's query heads)
+  const int64_t group = h / kv;
+  if (tq > 0 && group > 1 && (q->ld_head >= (int64_t(1) << 30) / group ||
+                              dout->ld_head >= (int64_t(1) << 30) / group))
+    return ZF_EINVAL;
+  const Span sl = span(lse, h, tq, tq, 4, ok);
+  Span sw;
+  const SequenceSpans ss = sequence_spans(*a);
+  const zf_status st_ws =
+      workspace_span(ws, ws_bytes, zf_attention_backward_workspace_bytes(a), ok, sw);
+  if (st_ws != ZF_OK) return st_ws;
+  // (the gradients may be columns of one buffer: apart from each other element by element)
+  if (!disjoint({sdq, sw}, {sq, sk, sv, so, sdo, sl, ss.q, ss.k}) ||
+      !disjoint({sdk, sw}, {sq, sk, sv, so, sdo, sl, ss.q, ss.k}) ||
+      !disjoint({sdv, sw}, {sq, sk, sv, so, sdo, sl, ss.q, ss.k}) ||
+      !heads_apart(dq, tq, h, dk, tk, kv, d) || !heads_apart(dq, tq, h, dv, tk, kv, d) ||
+      !heads_apart(dk, tk, kv, dv, tk, kv, d))
+    return ZF_EINVAL;
+  if (tq == 0 && tk == 0) return ZF_OK;
+  zf::AttentionBwdArgs args = attention_bwd_args(*a);
+  args.q = heads_arg(q);
+  args.k = heads_arg(k);
+  args.v = heads_arg(v);
+  args.out = heads_arg(out);
+  args.dout = heads_arg(dout);
+  args.dq = heads_arg(dq);
+  args.dk = heads_arg(dk);
+  args.dv = heads_arg(dv);
+  args.lse = lse;
+  return done(zf::launch_attention_backward(args, ws, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -13,6 +13,7 @@
 // that counts (matmul_rows_kernel; 1 x 11008 x 4096: 45 MB in 11.8 us, 3.8 TB/s).
 #include <algorithm>
 
+#include "zf_activation.hpp"
 #include "zf_layer.hpp"
 
 namespace zf {
@@ -158,6 +159,65 @@ __device__ __forceinline__ void store_units(float* out, u32x4 v, int64_t valid) 
   }
 }
 
+// What follows a linear layer's product, for 8 consecutive columns (c a multiple
+// of 8) of a row: t is the sums plus bias.  Every lane of a 16-lane group calls
+// it with a 128-column group of one row (the 8-bit output's largest magnitude is
+// theirs); valid: columns that exist, 0 also for a row that does not.
+template <typename T, int ACT>
+__device__ __forceinline__ void epilogue(const Epilogue& e, int64_t row, int64_t c, int64_t valid,
+                                         float (&t)[8], const Vec8<T>& res) {
+  Vec8<T> o;
+  if (e.z != nullptr) {
+    o.set(t);
+    o.template store<true>(static_cast<T*>(e.z) + row * e.ld_z + c, valid);
+  }
+  if (e.y == nullptr && e.q.data == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    t[j] = activate<ACT>(t[j]);
+    if (e.residual != nullptr) t[j] += res[j];
+    if (j >= valid) t[j] = 0.0f;
+  }
+  o.set(t);
+  if (e.y != nullptr) o.template store<true>(static_cast<T*>(e.y) + row * e.ld_y + c, valid);
+  if (e.q.data != nullptr) {
+    const uint32_t code = fp8_code(max16(abs_max(o)));
+    if (valid > 0) {
+      store_bytes8(e.q.data + row * e.q.ld + c, valid, quant8(o, code));
+      if (c % kFp8Group == 0) e.q.scale[row * e.q.ld_scale + c / kFp8Group] = static_cast<uint8_t>(code);
+    }
+  }
+}
+
+// 8 elements of the bias, zeros without one.
+__device__ __forceinline__ void load_bias(const Epilogue& e, int64_t n, int64_t c, float (&b)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) b[j] = 0.0f;
+  if (e.bias == nullptr) return;
+  if (e.bias_f32) {
+    Vec8<float> v;
+    v.load(static_cast<const float*>(e.bias) + c, n - c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[j] = v[j];
+  } else {
+    Vec8<uint16_t> v;
+    v.load(static_cast<const uint16_t*>(e.bias) + c, n - c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[j] = v[j];
+  }
+}
+
+// Marks the tile kernel's results as going through epilogue<T, ACT>.
+template <typename T, int ACT>
+struct Linear {
+  typedef T type;
+  static constexpr int act = ACT;
+};
+template <typename Out>
+struct IsLinear : std::false_type {};
+template <typename T, int ACT>
+struct IsLinear<Linear<T, ACT>> : std::true_type {};
+
 // A 256-thread block computes a 128 x 128 tile, each wave a quarter of it, from two
 // slots of 128 elements of the reduction in LDS.  Each half of a step multiplies
 // 64 elements from registers while the next 64 are read from LDS.  Memory is
@@ -171,7 +231,7 @@ __device__ __forceinline__ void store_units(float* out, u32x4 v, int64_t valid) 
 // bf16 and the sums can hold does not depend on where the scales lie.  PART: the
 // results are a share's, in fp32.
 template <typename Out, bool PART>
-__global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
+__global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p, Epilogue ep) {
   constexpr int kRows = kBM + kBN;
   constexpr int kSlot = kRows * kBK;
   constexpr int kLoads = 2 * kParts + 1;  // of a wave per step: 8 rows each, and 64 rows' codes
@@ -365,6 +425,52 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
   }
   wait_loads<0>();  // nothing lands in LDS from here on
 
+  if constexpr (IsLinear<Out>::value) {
+    // 32 rows of every wave's tile at a time through LDS: 64 rows of all 128 columns
+    // are a scale group of the 8-bit output each, 16 lanes of 8 columns.
+    typedef typename Out::type T;
+    constexpr int kPitch = kBN + 4;
+    static_assert(64 * kPitch * 4 <= 2 * kSlot, "the slab fits the slots");
+    float* const slab = reinterpret_cast<float*>(lds);
+    const int cg = 8 * (t & 15);
+    const int64_t c = n0 + cg, cols = p.n - c;
+    float bias[8];
+    load_bias(ep, p.n, c, bias);
+    int top[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top[e] = tops[kBM + cg + e];
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) {
+      __syncthreads();  // (the slots', or the last rows', readers are done)
+#pragma unroll
+      for (int j = 0; j < kTN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<v4f*>(slab + ((wave & 1) * 32 + (lane & 31)) * kPitch + wn + 32 * j +
+                                  2 * e + 4 * (lane >> 5)) =
+              v4f{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+      __syncthreads();
+#pragma unroll 1
+      for (int r = t >> 4; r < 64; r += 16) {
+        const int in = (r >> 5) * kWM + 32 * i + (r & 31);  // the tile's row
+        const int64_t row = m0 + in, valid = row < p.m ? cols : 0;
+        Vec8<T> res;
+        if (ep.residual != nullptr)
+          res.load(static_cast<const T*>(ep.residual) + row * ep.ld_residual + c, valid);
+        const int row_top = tops[in];
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const v4f w = *reinterpret_cast<const v4f*>(slab + r * kPitch + cg + e);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            v[e + q] = __builtin_ldexpf(w[q], row_top + top[e + q]) + bias[e + q];
+        }
+        epilogue<T, Out::act>(ep, row, c, valid, v, res);
+      }
+    }
+    return;
+  } else {
   // A lane holds 4 consecutive columns of a row at a time; through LDS, 32
   // rows of the wave's tile at a time, the rows become contiguous.  (Scaled on their
   // way out, in a loop: as they are written, each of 64 results in code of its own,
@@ -412,6 +518,33 @@ __global__ __launch_bounds__(256, 1) void matmul_tile_kernel(MatmulArgs p) {
     }
     __builtin_amdgcn_wave_barrier();
   }
+  }
+}
+
+// The epilogue of the sum of `shares` partial results (as below), 16 rows of a
+// 128-column group a block.
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void linear_join_kernel(const float* __restrict__ part,
+                                                          int32_t shares, int64_t m, int64_t n,
+                                                          Epilogue ep) {
+  const int64_t groups = (n + 127) / 128, size = m * n;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) / groups * 16 + (threadIdx.x >> 4);
+  const int64_t c = static_cast<int64_t>(blockIdx.x) % groups * 128 + 8 * (threadIdx.x & 15);
+  const int64_t valid = row < m ? n - c : 0;
+  Vec8<T> res;
+  if (ep.residual != nullptr)
+    res.load(static_cast<const T*>(ep.residual) + row * ep.ld_residual + c, valid);
+  float v[8] = {}, bias[8];
+  for (int32_t q = 0; q < shares; ++q) {
+    Vec8<float> w;
+    w.load(part + q * size + row * n + c, valid);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = q == 0 ? w[j] : v[j] + w[j];
+  }
+  load_bias(ep, n, c, bias);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] += bias[j];
+  epilogue<T, ACT>(ep, row, c, valid, v, res);
 }
 
 // out = the sum of `shares` partial results, in order (row by row of n, which
@@ -459,7 +592,7 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const float* __restric
 // products: b's rows along the accumulator's registers, a's along its lanes.  Each
 // group's sum is multiplied by its scales, in fp32.
 template <int W, int U, typename Out>
-__global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p) {
+__global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p, Epilogue ep) {
   __shared__ float sums[W][4][64];
   const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
@@ -525,7 +658,27 @@ __global__ __launch_bounds__(64 * W) void matmul_rows_kernel(MatmulArgs p) {
     for (int w = 1; w < W; ++w) v += sums[w][e][l];
     if (row < p.m && n0 + col < p.n) {
       const int64_t at = row * p.ld_out + n0 + col;
-      if constexpr (sizeof(Out) == 4) static_cast<float*>(p.out)[at] = v;
+      if constexpr (IsLinear<Out>::value) {
+        typedef typename Out::type T;
+        const int64_t c = n0 + col;
+        if (ep.bias != nullptr)
+          v += ep.bias_f32 ? static_cast<const float*>(ep.bias)[c]
+                           : widen_bf16(static_cast<const uint16_t*>(ep.bias)[c]);
+        const auto put = [&](void* o, int64_t ld) {
+          if constexpr (sizeof(T) == 4) static_cast<float*>(o)[row * ld + c] = v;
+          else static_cast<uint16_t*>(o)[row * ld + c] = round_bf16(v);
+        };
+        if (ep.z != nullptr) put(ep.z, ep.ld_z);
+        if (ep.y != nullptr) {
+          v = activate<Out::act>(v);
+          if (ep.residual != nullptr) {
+            const T r = static_cast<const T*>(ep.residual)[row * ep.ld_residual + c];
+            if constexpr (sizeof(T) == 4) v += r;
+            else v += widen_bf16(r);
+          }
+          put(ep.y, ep.ld_y);
+        }
+      } else if constexpr (sizeof(Out) == 4) static_cast<float*>(p.out)[at] = v;
       else static_cast<uint16_t*>(p.out)[at] = round_bf16(v);
     }
   }
@@ -564,10 +717,10 @@ int shares(int64_t m, int64_t n, int64_t k) {
 }
 
 template <typename Out>
-void launch_rows(const MatmulArgs& a, hipStream_t s) {
+void launch_rows(const MatmulArgs& a, const Epilogue& e, hipStream_t s) {
 #define ZF_ROWS(W, U)                                                                   \
   hipLaunchKernelGGL((matmul_rows_kernel<W, U, Out>), dim3(static_cast<uint32_t>(blocks)), \
-                     dim3(64 * W), 0, s, a)
+                     dim3(64 * W), 0, s, a, e)
   const int64_t blocks = (a.n + 15) / 16;
   if (blocks >= 512) ZF_ROWS(4, 8);
   else if (blocks >= 128) ZF_ROWS(8, 4);
@@ -575,24 +728,63 @@ void launch_rows(const MatmulArgs& a, hipStream_t s) {
 #undef ZF_ROWS
 }
 
-template <typename Out>
-void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(tiles(a.m, a.n)));
-  const int q = shares(a.m, a.n, a.k);
-  if (q == 1) {
-    hipLaunchKernelGGL((matmul_tile_kernel<Out, false>), grid, dim3(256), 0, s, a);
-    return;
-  }
+int64_t share_of(int64_t k, int q) {
+  const int64_t steps = (k + kBK - 1) / kBK;
+  return ((steps + q - 1) / q + 3) / 4 * 4;
+}
+// The q shares' partial results, in ws.
+void launch_shares(const MatmulArgs& a, int q, void* ws, hipStream_t s) {
   MatmulArgs b = a;
   b.out = ws;
   b.ld_out = a.n;
-  const int64_t steps = (a.k + kBK - 1) / kBK;
-  b.share = static_cast<int32_t>(((steps + q - 1) / q + 3) / 4 * 4);
-  hipLaunchKernelGGL((matmul_tile_kernel<float, true>), dim3(grid.x, q), dim3(256), 0, s, b);
+  b.share = static_cast<int32_t>(share_of(a.k, q));
+  hipLaunchKernelGGL((matmul_tile_kernel<float, true>),
+                     dim3(static_cast<uint32_t>(tiles(a.m, a.n)), q), dim3(256), 0, s, b, Epilogue{});
+}
+
+template <typename Out>
+void launch_tiles(const MatmulArgs& a, void* ws, hipStream_t s) {
+  const int q = shares(a.m, a.n, a.k);
+  if (q == 1) {
+    hipLaunchKernelGGL((matmul_tile_kernel<Out, false>), dim3(static_cast<uint32_t>(tiles(a.m, a.n))),
+                       dim3(256), 0, s, a, Epilogue{});
+    return;
+  }
+  launch_shares(a, q, ws, s);
   const int64_t blocks = (a.m * a.n + 2047) / 2048;
   hipLaunchKernelGGL((matmul_join_kernel<Out>), dim3(static_cast<uint32_t>(std::min<int64_t>(blocks, 2048))),
                      dim3(256), 0, s, static_cast<const float*>(ws), q, a.m, a.n,
                      static_cast<Out*>(a.out), a.ld_out);
+}
+
+template <typename T, int ACT>
+void launch_linear(const MatmulArgs& a, const Epilogue& e, void* ws, hipStream_t s) {
+  const auto join = [&](int q) {
+    hipLaunchKernelGGL((linear_join_kernel<T, ACT>),
+                       dim3(static_cast<uint32_t>((a.m + 15) / 16 * ((a.n + 127) / 128))), dim3(256), 0,
+                       s, static_cast<const float*>(ws), q, a.m, a.n, e);
+  };
+  if (takes_rows(a.m, a.n)) {
+    if (e.q.data == nullptr) {
+      launch_rows<Linear<T, ACT>>(a, e, s);
+      return;
+    }
+    // (a scale group spans 8 blocks of 16 columns)
+    MatmulArgs b = a;
+    b.out = ws;
+    b.ld_out = a.n;
+    launch_rows<float>(b, Epilogue{}, s);
+    join(1);
+    return;
+  }
+  const int q = shares(a.m, a.n, a.k);
+  if (q == 1) {
+    hipLaunchKernelGGL((matmul_tile_kernel<Linear<T, ACT>, false>),
+                       dim3(static_cast<uint32_t>(tiles(a.m, a.n))), dim3(256), 0, s, a, e);
+    return;
+  }
+  launch_shares(a, q, ws, s);
+  join(q);
 }
 
 }  // namespace
@@ -605,12 +797,27 @@ size_t matmul_workspace(int64_t m, int64_t n, int64_t k) {
 hipError_t launch_matmul(const MatmulArgs& a, void* ws, hipStream_t s) {
   (void)hipGetLastError();
   if (takes_rows(a.m, a.n)) {
-    if (a.out_f32) launch_rows<float>(a, s);
-    else launch_rows<uint16_t>(a, s);
+    if (a.out_f32) launch_rows<float>(a, Epilogue{}, s);
+    else launch_rows<uint16_t>(a, Epilogue{}, s);
   } else {
     if (a.out_f32) launch_tiles<float>(a, ws, s);
     else launch_tiles<uint16_t>(a, ws, s);
   }
+  return hipGetLastError();
+}
+
+size_t linear_workspace(int64_t m, int64_t n, int64_t k, bool q) {
+  if (takes_rows(m, n)) return q ? static_cast<size_t>(m) * n * sizeof(float) : 0;
+  return matmul_workspace(m, n, k);
+}
+
+hipError_t launch_linear(const MatmulArgs& a, const Epilogue& e, int32_t dtype, void* ws,
+                         hipStream_t s) {
+  (void)hipGetLastError();
+  with_activation(e.activation, [&](auto act) {
+    if (dtype == ZF_F32) launch_linear<float, act>(a, e, ws, s);
+    else launch_linear<uint16_t, act>(a, e, ws, s);
+  });
   return hipGetLastError();
 }
 

@@ -20,54 +20,10 @@
 // depend on timing.
 #include <algorithm>
 
-#include "zf_layer.hpp"
+#include "zf_norm.hpp"
 
 namespace zf {
 namespace {
-
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-  return x;
-}
-
-// The block's sum of x, in every thread.  `red` may be used again after the
-// next block_sum or barrier (two buffers, alternated by the caller).
-template <int NT>
-__device__ __forceinline__ float block_sum(float x, float (&red)[NT / 64]) {
-  x = wave_sum(x);
-  if constexpr (NT == 64) return x;
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
-  float s = red[0];
-#pragma unroll
-  for (int w = 1; w < NT / 64; ++w) s += red[w];
-  return s;
-}
-
-template <typename Args>
-__device__ __forceinline__ void load_gain(const Args& a, int64_t c, float (&g)[8]) {
-  if (a.gain_f32) {
-    Vec8<float> v;
-    v.load(static_cast<const float*>(a.gain) + c, a.cols - c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = v[j];
-  } else {
-    Vec8<uint16_t> v;
-    v.load(static_cast<const uint16_t*>(a.gain) + c, a.cols - c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = v[j];
-  }
-}
-
-// x + residual, rounded to the storage type.
-template <typename T>
-__device__ __forceinline__ void add(Vec8<T>& x, const Vec8<T>& r) {
-  float s[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) s[j] = x[j] + r[j];
-  x.set(s);
-}
 
 // y of 8 elements written, in its own type and in 8 bits.  Every lane of a
 // 16-lane group calls it (the group's largest magnitude is theirs); elements
@@ -167,13 +123,6 @@ __global__ __launch_bounds__(NT) void rmsnorm_wide_kernel(NormArgs a) {
       store_y(a, row, c, h, rstd);
     }
   }
-}
-
-// Rows [r0, r1) of backward block b of `blocks`.
-__device__ __forceinline__ void block_rows(int64_t rows, int64_t blocks, int64_t b, int64_t& r0,
-                                           int64_t& r1) {
-  r0 = rows * b / blocks;
-  r1 = rows * (b + 1) / blocks;
 }
 
 // The next row is loaded while the present one is reduced, where the registers
@@ -315,15 +264,18 @@ __global__ __launch_bounds__(NT) void rmsnorm_dx_wide_kernel(NormBwdArgs a) {
   }
 }
 
-// dgain[j] = the sum of column j's `parts` partials: each of the block's shares a
+// out[j] = the sum of column j's `parts` partials: each of the block's shares a
 // contiguous range of them in order, eight loads in flight, then the shares in
 // order.  Columns per block: 32 are one line of a partial sum's row; 64 leave a
 // join of 384 columns to 6 blocks (8192 x 384: 19 us against 15 with the sums).
 constexpr int kJoinCols = 32, kJoinShares = 1024 / kJoinCols;
-__global__ __launch_bounds__(1024) void dgain_kernel(const float* __restrict__ part,
-                                                     int64_t parts, int64_t cols,
-                                                     float* __restrict__ dgain) {
+__global__ __launch_bounds__(1024) void join_columns_kernel(const float* __restrict__ part,
+                                                            int64_t parts, int64_t cols,
+                                                            float* __restrict__ out0,
+                                                            float* __restrict__ out1) {
   __shared__ float red[kJoinShares][kJoinCols];
+  float* const out = blockIdx.y == 0 ? out0 : out1;
+  part += blockIdx.y * parts * cols;
   const int lane = threadIdx.x % kJoinCols, share = threadIdx.x / kJoinCols;
   const int64_t p1 = parts * (share + 1) / kJoinShares;
   for (int64_t c0 = static_cast<int64_t>(blockIdx.x) * kJoinCols; c0 < cols;
@@ -343,32 +295,12 @@ __global__ __launch_bounds__(1024) void dgain_kernel(const float* __restrict__ p
     if (share == 0 && c < cols) {
 #pragma unroll
       for (int w = 1; w < kJoinShares; ++w) s += red[w][lane];
-      dgain[c] = s;
+      out[c] = s;
     }
     __syncthreads();
   }
 }
 
-constexpr int64_t kMaxGrid = int64_t(1) << 21;  // blocks; a dispatch holds fewer than 2^32 threads
-constexpr int64_t kWideCols = 1024 * 8 * 2;  // the widest row kept in registers
-
-// f(threads, pieces a thread) with the fewest threads that hold a row.
-template <typename F>
-auto with_shape(int64_t cols, F&& f) {
-#define ZF_SHAPE(NT, V) \
-  if (cols <= NT * V * 8) return f(std::integral_constant<int, NT>(), std::integral_constant<int, V>())
-  ZF_SHAPE(64, 1);
-  ZF_SHAPE(128, 1);
-  ZF_SHAPE(256, 1);
-  ZF_SHAPE(384, 1);
-  ZF_SHAPE(512, 1);
-  ZF_SHAPE(640, 1);
-  ZF_SHAPE(768, 1);
-  ZF_SHAPE(1024, 1);
-  ZF_SHAPE(768, 2);
-#undef ZF_SHAPE
-  return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
-}
 int backward_threads(int64_t cols) {
   return with_shape(cols, [](auto nt, auto) { return static_cast<int>(nt); });
 }
@@ -443,6 +375,15 @@ hipError_t launch_rmsnorm(const NormArgs& a, int32_t dtype, hipStream_t s) {
   return hipGetLastError();
 }
 
+void launch_join_columns(const float* part, int64_t parts, int64_t cols, float* out0, float* out1,
+                         hipStream_t s) {
+  hipLaunchKernelGGL(
+      join_columns_kernel,
+      dim3(static_cast<uint32_t>(std::min<int64_t>((cols + kJoinCols - 1) / kJoinCols, kMaxGrid)),
+           out1 != nullptr ? 2 : 1),
+      dim3(1024), 0, s, part, parts, cols, out0, out1);
+}
+
 size_t rmsnorm_backward_workspace(int64_t rows, int64_t cols) {
   return static_cast<size_t>(backward_blocks(rows, cols)) * static_cast<size_t>(cols) * sizeof(float);
 }
@@ -454,10 +395,7 @@ hipError_t launch_rmsnorm_backward(const NormBwdArgs& a, int32_t dtype, hipStrea
     else norm_backward<float>(a, s);
   }
   if (a.dgain != nullptr)  // (no rows: no partials, zeros)
-    hipLaunchKernelGGL(
-        dgain_kernel,
-        dim3(static_cast<uint32_t>(std::min<int64_t>((a.cols + kJoinCols - 1) / kJoinCols, kMaxGrid))),
-        dim3(1024), 0, s, a.part, backward_blocks(a.rows, a.cols), a.cols, a.dgain);
+    launch_join_columns(a.part, backward_blocks(a.rows, a.cols), a.cols, a.dgain, nullptr, s);
   return hipGetLastError();
 }
 

@@ -19,8 +19,8 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
-from ._lib import (LIB, AdamHparams, ZfAdamwTensor, ZfFp8, _check, _empty, _mat, _ptr, _stream,
-                   _vec, _workspace, c_sz, c_vp)
+from ._lib import (LIB, AdamHparams, ZfAdamwTensor, ZfEpilogue, ZfFp8, _check, _empty, _mat, _ptr,
+                   _same_device, _stream, _vec, _workspace, c_sz, c_vp)
 
 DTYPES = {torch.bfloat16: 0, torch.float32: 1}  # zf_dtype
 DATA, SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
@@ -260,6 +260,280 @@ def rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, rstd
         ld_res, _ptr(dx), ld_dx, _ptr(dgain), _ptr(workspace),
         _workspace(workspace), _stream(stream)))
     return dx, dgain
+
+
+# ---- layer norm -------------------------------------------------------------------
+
+class LayerNorm(NamedTuple):
+    """What layernorm returns; y, q: None where not wanted; h: x itself without a
+    residual."""
+    y: Optional[torch.Tensor]
+    h: torch.Tensor
+    mean: torch.Tensor
+    rstd: torch.Tensor
+    q: Optional[Fp8]
+
+
+def _fp8_parts(**named):
+    """The tensors of 8-bit operands, for _same_device."""
+    out = {}
+    for name, f in named.items():
+        if f is not None:
+            out[name + ".data"], out[name + ".scale"] = f.data, f.scale
+    return out
+
+
+def layernorm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor] = None,
+              residual: Optional[torch.Tensor] = None, eps: float = 1e-5, want_y: bool = True,
+              want_q: bool = False, h: Optional[torch.Tensor] = None,
+              y: Optional[torch.Tensor] = None, q: Optional[Fp8] = None,
+              mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+              stream=None) -> LayerNorm:
+    """h = x + residual, y = (h - mean(h)) / std(h) * gain + bias, in x's type
+    and/or in 8 bits (zf_layernorm_forward).  x, residual [rows, cols] bf16 or
+    fp32; gain, bias [cols] bf16 or fp32, both of one type.  h may be the
+    residual's (or x's) own tensor; outputs that are not given are allocated."""
+    dt = _dtype(x, "x")
+    ld = _mat(x, x.dtype, "x")
+    r, c = x.shape
+    gdt = _dtype(gain, "gain")
+    _vec(gain, gain.dtype, "gain", c)
+    if bias is not None:
+        _vec(bias, gain.dtype, "bias", c)
+    dtype, dev = x.dtype, x.device
+    _same_device(stream, x=x, gain=gain, bias=bias, residual=residual, h=h, y=y, mean=mean,
+                 rstd=rstd, **_fp8_parts(q=q))
+    if mean is None:
+        mean = _empty(r, torch.float32, dev, stream)
+    else:
+        _vec(mean, torch.float32, "mean", r)
+    if rstd is None:
+        rstd = _empty(r, torch.float32, dev, stream)
+    else:
+        _vec(rstd, torch.float32, "rstd", r)
+    ld_res, ld_h, ld_y, c_q = 0, c, c, None
+    if residual is not None:
+        ld_res = _mat(residual, dtype, "residual", r, c)
+    if h is not None:
+        ld_h = _mat(h, dtype, "h", r, c)
+    elif residual is not None:
+        h = _empty((r, c), dtype, dev, stream)
+    if y is not None:
+        ld_y = _mat(y, dtype, "y", r, c)
+    elif want_y:
+        y = _empty((r, c), dtype, dev, stream)
+    if q is not None:
+        c_q = q.as_c("q", r, c)
+    elif want_q:
+        q, c_q = _alloc_fp8(r, c, 1, dev, stream)
+    _check("zf_layernorm_forward", LIB.zf_layernorm_forward(
+        _ptr(x), ld, _ptr(residual), ld_res, dt, r, c, _ptr(gain), _ptr(bias), gdt, float(eps),
+        _ptr(h), ld_h, _ptr(y), ld_y, ctypes.byref(c_q) if c_q is not None else None, _ptr(mean),
+        _ptr(rstd), _stream(stream)))
+    return LayerNorm(y, x if h is None else h, mean, rstd, q)
+
+
+def layernorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return LIB.zf_layernorm_backward_workspace_bytes(rows, cols)
+
+
+def layernorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, mean: torch.Tensor,
+                       rstd: torch.Tensor, dresidual: Optional[torch.Tensor] = None,
+                       dx: Optional[torch.Tensor] = None, dgain: Optional[torch.Tensor] = None,
+                       dbias: Optional[torch.Tensor] = None, want_dgain: bool = True,
+                       want_dbias: bool = True, workspace: Optional[torch.Tensor] = None,
+                       stream=None
+                       ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dx, dgain, dbias) of layernorm, from its h, mean and rstd
+    (zf_layernorm_backward).  dx is the gradient of x and of the residual;
+    dresidual, the gradient that reaches h from elsewhere, is added to it.  dx
+    may be dy's or dresidual's own tensor.  dgain and dbias are fp32 [cols]."""
+    dt = _dtype(dy, "dy")
+    ld_dy = _mat(dy, dy.dtype, "dy")
+    r, c = dy.shape
+    ld_h = _mat(h, dy.dtype, "h", r, c)
+    gdt = _dtype(gain, "gain")
+    _vec(gain, gain.dtype, "gain", c)
+    _vec(mean, torch.float32, "mean", r)
+    _vec(rstd, torch.float32, "rstd", r)
+    _same_device(stream, dy=dy, h=h, gain=gain, mean=mean, rstd=rstd, dresidual=dresidual, dx=dx,
+                 dgain=dgain, dbias=dbias, workspace=workspace)
+    ld_res = 0
+    if dresidual is not None:
+        ld_res = _mat(dresidual, dy.dtype, "dresidual", r, c)
+    if dx is None:
+        dx, ld_dx = _empty((r, c), dy.dtype, dy.device, stream), c
+    else:
+        ld_dx = _mat(dx, dy.dtype, "dx", r, c)
+    if dgain is not None:
+        _vec(dgain, torch.float32, "dgain", c)
+    elif want_dgain:
+        dgain = _empty(c, torch.float32, dy.device, stream)
+    if dbias is not None:
+        _vec(dbias, torch.float32, "dbias", c)
+    elif want_dbias:
+        dbias = _empty(c, torch.float32, dy.device, stream)
+    if workspace is None and (dgain is not None or dbias is not None):
+        need = LIB.zf_layernorm_backward_workspace_bytes(r, c)
+        workspace = _empty(need, torch.uint8, dy.device, stream) if need else None
+    _check("zf_layernorm_backward", LIB.zf_layernorm_backward(
+        _ptr(dy), ld_dy, _ptr(h), ld_h, dt, r, c, _ptr(gain), gdt, _ptr(mean), _ptr(rstd),
+        _ptr(dresidual), ld_res, _ptr(dx), ld_dx, _ptr(dgain), _ptr(dbias), _ptr(workspace),
+        _workspace(workspace), _stream(stream)))
+    return dx, dgain, dbias
+
+
+# ---- a linear layer's product with its epilogue ---------------------------------------
+
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}  # zf_activation
+
+
+def _activation(name: Optional[str]) -> int:
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation is one of {list(ACTIVATIONS)}, got {name!r}")
+    return ACTIVATIONS[name]
+
+
+class LinearFp8(NamedTuple):
+    """What linear_fp8 returns; None where not wanted."""
+    y: Optional[torch.Tensor]
+    z: Optional[torch.Tensor]
+    q: Optional[Fp8]
+
+
+def linear_fp8_workspace_bytes(m: int, n: int, k: int, q: bool = False) -> int:
+    """Workspace bytes of linear_fp8; q: its 8-bit output is wanted."""
+    return LIB.zf_linear_fp8_workspace_bytes(m, n, k, int(q))
+
+
+def linear_fp8(a: Fp8, b: Fp8, bias: Optional[torch.Tensor] = None,
+               activation: Optional[str] = None, residual: Optional[torch.Tensor] = None,
+               want_y: bool = True, want_z: bool = False, want_q: bool = False,
+               y: Optional[torch.Tensor] = None, z: Optional[torch.Tensor] = None,
+               q: Optional[Fp8] = None, dtype=torch.bfloat16,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> LinearFp8:
+    """matmul_fp8 with a linear layer's epilogue in it (zf_linear_fp8):
+    z = a @ b.T + bias, y = act(z) + residual, q = y in 8 bits, each where asked
+    for.  activation: None, "relu", "gelu", "gelu_tanh" or "silu".  bias [n]
+    bf16 or fp32; residual, y, z [m, n] of one type, bf16 or fp32 (`dtype`
+    where none is given).  y may be the residual's own tensor.  z is what
+    linear_fp8_backward takes."""
+    m, k = a.data.shape
+    n = b.data.shape[0]
+    c_a, c_b = a.as_c("a"), b.as_c("b", None, k)
+    dev = a.data.device
+    _same_device(stream, **_fp8_parts(a=a, b=b, q=q), bias=bias, residual=residual, y=y, z=z,
+                 workspace=workspace)
+    for t in (residual, y, z):
+        if t is not None:
+            dtype = t.dtype
+            break
+    code = DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"dtype: expected bfloat16 or float32, got {dtype}")
+    e = ZfEpilogue(dtype=code, activation=_activation(activation), ld_residual=n, ld_z=n, ld_y=n)
+    if bias is not None:
+        e.bias_dtype = _dtype(bias, "bias")
+        _vec(bias, bias.dtype, "bias", n)
+        e.bias = _ptr(bias)
+    if residual is not None:
+        e.ld_residual = _mat(residual, dtype, "residual", m, n)
+        e.residual = _ptr(residual)
+    if y is not None:
+        e.ld_y = _mat(y, dtype, "y", m, n)
+    elif want_y:
+        y = _empty((m, n), dtype, dev, stream)
+    if z is not None:
+        e.ld_z = _mat(z, dtype, "z", m, n)
+    elif want_z:
+        z = _empty((m, n), dtype, dev, stream)
+    c_q = None
+    if q is not None:
+        c_q = q.as_c("q", m, n)
+    elif want_q:
+        q, c_q = _alloc_fp8(m, n, 1, dev, stream)
+    if y is None and z is None and q is None:
+        raise ValueError("no output is wanted")
+    e.y, e.z = _ptr(y), _ptr(z)
+    if c_q is not None:
+        e.q = ctypes.pointer(c_q)
+    if m and n:
+        need = LIB.zf_linear_fp8_workspace_bytes(m, n, k, int(q is not None))
+        if workspace is None and need:
+            workspace = _empty(need, torch.uint8, dev, stream)
+        _check("zf_linear_fp8", LIB.zf_linear_fp8(
+            ctypes.byref(c_a), ctypes.byref(c_b), m, n, k, ctypes.byref(e), _ptr(workspace),
+            _workspace(workspace), _stream(stream)))
+    return LinearFp8(y, z, q)
+
+
+class LinearFp8Grad(NamedTuple):
+    """What linear_fp8_backward returns; None where not wanted."""
+    dz: Optional[torch.Tensor]
+    q: Optional[Fp8]
+    qt: Optional[Fp8]
+    dbias: Optional[torch.Tensor]
+
+
+def linear_fp8_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return LIB.zf_linear_fp8_backward_workspace_bytes(rows, cols)
+
+
+def linear_fp8_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None,
+                        activation: Optional[str] = None, rows: bool = True,
+                        transposed: bool = True, want_dz: bool = False, want_dbias: bool = True,
+                        dz: Optional[torch.Tensor] = None, q: Optional[Fp8] = None,
+                        qt: Optional[Fp8] = None, dbias: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> LinearFp8Grad:
+    """The gradient at linear_fp8's product, dz = dy * act'(z), in one pass
+    (zf_linear_fp8_backward): in 8 bits for the input gradient's product
+    (`rows`: q) and the weight gradient's (`transposed`: qt), the bias's
+    gradient (dbias, fp32 [cols]), and dz itself where it is wanted.  dy
+    [rows, cols] bf16 or fp32, z (not needed without an activation) of the same
+    type.  Then dx = matmul_fp8(q, wt), dw = matmul_fp8(qt, xt); the residual's
+    gradient is dy.  dz may be dy's or z's own tensor."""
+    dt = _dtype(dy, "dy")
+    ld = _mat(dy, dy.dtype, "dy")
+    r, c = dy.shape
+    act = _activation(activation)
+    ld_z = c
+    if act:
+        if z is None:
+            raise ValueError("z: needed with an activation")
+        ld_z = _mat(z, dy.dtype, "z", r, c)
+    else:
+        z = None
+    _same_device(stream, dy=dy, z=z, dz=dz, dbias=dbias, workspace=workspace,
+                 **_fp8_parts(q=q, qt=qt))
+    ld_dz, c_q, c_qt = c, None, None
+    if dz is not None:
+        ld_dz = _mat(dz, dy.dtype, "dz", r, c)
+    elif want_dz:
+        dz = _empty((r, c), dy.dtype, dy.device, stream)
+    if q is not None:
+        c_q = q.as_c("q", r, c)
+    elif rows:
+        q, c_q = _alloc_fp8(r, c, 1, dy.device, stream)
+    if qt is not None:
+        c_qt = qt.as_c("qt", c, r)
+    elif transposed:
+        qt, c_qt = _alloc_fp8(c, r, 1, dy.device, stream)
+    if dbias is not None:
+        _vec(dbias, torch.float32, "dbias", c)
+    elif want_dbias:
+        dbias = _empty(c, torch.float32, dy.device, stream)
+    if dz is None and q is None and qt is None and dbias is None:
+        raise ValueError("no output is wanted")
+    if dbias is not None and workspace is None:
+        need = LIB.zf_linear_fp8_backward_workspace_bytes(r, c)
+        workspace = _empty(need, torch.uint8, dy.device, stream) if need else None
+    if c and (r or dbias is not None):
+        _check("zf_linear_fp8_backward", LIB.zf_linear_fp8_backward(
+            _ptr(dy), ld, _ptr(z), ld_z, dt, r, c, act, _ptr(dz), ld_dz,
+            ctypes.byref(c_q) if c_q is not None else None,
+            ctypes.byref(c_qt) if c_qt is not None else None, _ptr(dbias), _ptr(workspace),
+            _workspace(workspace), _stream(stream)))
+    return LinearFp8Grad(dz, q, qt, dbias)
 
 
 # ---- AdamW over many tensors -----------------------------------------------------------
