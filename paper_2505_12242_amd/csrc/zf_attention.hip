@@ -28,11 +28,11 @@ struct Rows {
   int32_t lim;   // keys that the lane's row sees
 };
 
-// One tile of keys, from key kb of the sequence on.  MASK: some row sees only
+// One tile of keys, from key kb of the sequence on.  mask: some row sees only
 // some of them.
-template <int DP, bool MASK>
+template <int DP>
 __device__ __forceinline__ void tile_step(Rows<DP>& w, const uint8_t* k, uint8_t* v, int32_t kb,
-                                          float c) {
+                                          bool mask, float c) {
   typedef Heads<DP> H;
   const int half = threadIdx.x >> 5 & 1;
   v16f s[2];
@@ -42,14 +42,19 @@ __device__ __forceinline__ void tile_step(Rows<DP>& w, const uint8_t* k, uint8_t
 #pragma unroll
     for (int j = 0; j < H::kChunks; ++j) s[t] = mma(H::frag(k, 32 * t, j), w.q[j], s[t]);
   }
+  __builtin_amdgcn_sched_barrier(0);
+  if (mask) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (kb + 32 * t + reg_row(r) + 4 * half >= w.lim) s[t][r] = -INFINITY;
+  }
   float top = -INFINITY;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (MASK && kb + 32 * t + reg_row(r) + 4 * half >= w.lim) s[t][r] = -INFINITY;
-      top = fmaxf(top, s[t][r]);
-    }
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
   top = fmaxf(top, other_half(top));
   // (the first tile that a row sees anything of has m = -infinity)
   if (__any(top * c > w.m * c + 8.0f)) {
@@ -83,7 +88,7 @@ __device__ __forceinline__ void tile_step(Rows<DP>& w, const uint8_t* k, uint8_t
 template <int DP, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
   typedef Heads<DP> H;
-  constexpr int kTile = kKeys * H::kPitch, kLoads = kKeys / H::kPer / 4;  // loads of a wave
+  constexpr int kTile = kKeys * H::kPitch;
   __shared__ __align__(1024) uint8_t lds[4 * kTile];  // two slots of k and v
   const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6);
   // the key head is the fastest: with a multiple of 8 of them an XCD's blocks
@@ -124,35 +129,17 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     end = min(end, begin + per);
   }
 
-  const uint32_t ldk = static_cast<uint32_t>(a.k.ld_token) * 2, ldv = static_cast<uint32_t>(a.v.ld_token) * 2;
-  const uint16_t* const kp = a.k.p + kvh * a.k.ld_head;
-  const uint16_t* const vp = a.v.p + kvh * a.v.ld_head;
-  const auto load = [&](int32_t kb, int slot) {
-    const int64_t t0 = static_cast<int64_t>(w.k0) + kb;
-    const rsrc_t rk = make_rsrc(kp + t0 * a.k.ld_token, -1), rv = make_rsrc(vp + t0 * a.v.ld_token, -1);
-    const int last = w.lk - 1 - kb;
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const int r = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
-      const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
-      const uint32_t row = static_cast<uint32_t>(min(r, last));
-      uint8_t* const p = lds + slot * 2 * kTile + (wave * kLoads + n) * 1024;
-      dma16(rk, p, row * ldk + unit * 16);
-      dma16(rv, p + kTile, row * ldv + unit * 16);
-    }
-  };
-
-  if (begin < end) load(begin, 0);
+  const KeyLoader<DP, kKeys, 4> keys(a, w, kvh, wave);
+  const uint32_t base = lds_offset(lds);
+  if (begin < end) keys.load(begin, base, wave);
+  settle(x.q);
   int slot = 0;
   for (int32_t kb = begin; kb < end; kb += kKeys) {
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    if (kb + kKeys < end) load(kb + kKeys, slot ^ 1);
+    wait_dma<0>();
+    if (kb + kKeys < end) keys.load(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
     const uint8_t* const k = lds + slot * 2 * kTile;
     uint8_t* const v = lds + slot * 2 * kTile + kTile;
-    if (kb < most) {
-      if (kb + kKeys > least) tile_step<DP, true>(x, k, v, kb, a.scale * kLog2E);
-      else tile_step<DP, false>(x, k, v, kb, a.scale * kLog2E);
-    }
+    if (kb < most) tile_step<DP>(x, k, v, kb, kb + kKeys > least, a.scale * kLog2E);
     slot ^= 1;
   }
 

@@ -185,12 +185,97 @@ __device__ __forceinline__ int32_t keys_of(const Args& a, const Sequence& w, int
   return a.causal ? max(min(w.lk, i + w.lk - w.lq + 1), 0) : w.lk;
 }
 
-// 16 bytes a lane from memory to LDS, at lds + lane * 16 (`lds` the same in
-// every lane).
-__device__ __forceinline__ void dma16(rsrc_t r, uint8_t* lds, uint32_t voff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16,
-                                           voff, 0, 0, 0);
+// 16 or 4 bytes a lane from memory to LDS, at byte `lds` + lane * 16 or 4 (`lds` the
+// same in every lane).  Written out because the compiler would wait for all of them
+// before the next transposing read of any part of LDS: the kernels wait
+// themselves, where a tile is needed.  Nothing is loaded to a register.
+__device__ __forceinline__ uint32_t lds_offset(const uint8_t* lds) {
+  return static_cast<uint32_t>(uniform_i32(static_cast<int32_t>(reinterpret_cast<uintptr_t>(
+      (const __attribute__((address_space(3))) uint8_t*)lds))));
 }
+__device__ __forceinline__ void dma16(rsrc_t r, uint32_t lds, uint32_t voff) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
+                   lds),
+               "v"(voff), "s"(r)
+               : "memory", "m0");
+#endif
+}
+__device__ __forceinline__ void dma4(rsrc_t r, uint32_t lds, uint32_t voff) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(
+                   lds),
+               "v"(voff), "s"(r)
+               : "memory", "m0");
+#endif
+}
+// Waits for a vector's loads here, in front of a loop, so that the loop does not
+// wait for loads at their first use (and with them for its own, one tile ahead).
+template <int N>
+__device__ __forceinline__ void settle(v8b (&x)[N]) {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+  for (int c = 0; c < N; ++c) asm volatile("" : "+v"(x[c]));
+#endif
+}
+// Waits until at most N of the wave's loads are in flight, then for the block's
+// other waves.
+template <int N>
+__device__ __forceinline__ void wait_dma() {
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// Loads tiles of N keys of k and v: the wave's part of each (`waves` of them load
+// together), rows past the last key repeating it, units past the head's width
+// the last one (the other operand is zero there, or the result not stored).
+template <int DP, int N, int WAVES>
+struct KeyLoader {
+  typedef Heads<DP> H;
+  static constexpr int kLoads = N / H::kPer / WAVES;  // of a wave, of either
+  static constexpr int kTile = N * H::kPitch;
+  const uint16_t *k, *v;
+  int64_t ldk, ldv;
+  uint32_t at[2][kLoads], unit[kLoads];
+  int32_t keys, row[kLoads];
+
+  template <typename Args>
+  __device__ __forceinline__ KeyLoader(const Args& a, const Sequence& w, int32_t kvh, int wave) {
+    const int lane = threadIdx.x & 63;
+    ldk = a.k.ld_token;
+    ldv = a.v.ld_token;
+    k = a.k.p + kvh * a.k.ld_head + w.k0 * ldk;
+    v = a.v.p + kvh * a.v.ld_head + w.k0 * ldv;
+    keys = w.lk;
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      row[n] = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
+      unit[n] = 16 * min((lane % H::kUnits) ^ H::swizzle(row[n]), a.dim / 8 - 1);
+      at[0][n] = offset(row[n], ldk) + unit[n];
+      at[1][n] = offset(row[n], ldv) + unit[n];
+    }
+  }
+  static __device__ __forceinline__ uint32_t offset(int32_t row, int64_t ld) {
+    return static_cast<uint32_t>(row) * (static_cast<uint32_t>(ld) * 2);
+  }
+  // Keys kb .. kb + N - 1 to byte `lds`, k's first, v's kTile behind them.  kb < keys.
+  __device__ __forceinline__ void load(int32_t kb, uint32_t lds, int wave) const {
+    const rsrc_t rk = make_rsrc(k + kb * ldk, -1), rv = make_rsrc(v + kb * ldv, -1);
+    lds += wave * kLoads * 1024;
+    if (kb + N <= keys) {
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) dma16(rk, lds + n * 1024, at[0][n]);
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n) dma16(rv, lds + kTile + n * 1024, at[1][n]);
+    } else {
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n)
+        dma16(rk, lds + n * 1024, offset(min(row[n], keys - 1 - kb), ldk) + unit[n]);
+#pragma unroll
+      for (int n = 0; n < kLoads; ++n)
+        dma16(rv, lds + kTile + n * 1024, offset(min(row[n], keys - 1 - kb), ldv) + unit[n]);
+    }
+  }
+};
 
 size_t attention_workspace(const AttentionArgs& a);
 hipError_t launch_attention(AttentionArgs a, void* ws, hipStream_t s);

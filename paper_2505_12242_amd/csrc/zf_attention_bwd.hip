@@ -56,7 +56,7 @@ __device__ __forceinline__ void store_vector(uint16_t* p, int dim, const v16f (&
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a) {
   typedef Heads<DP> H;
-  constexpr int kTile = kKeys * H::kPitch, kLoads = kKeys / H::kPer / 4;  // loads of a wave
+  constexpr int kTile = kKeys * H::kPitch;
   __shared__ __align__(1024) uint8_t lds[4 * kTile];  // two slots of k and v
   const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6), half = lane >> 5;
   const int32_t kvh = blockIdx.x % a.kv_heads;
@@ -83,7 +83,11 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
     delta += other_half(delta);
   }
   if (valid && lane < 32) a.delta[head * a.tokens_q + token] = delta;
-  const float lse = a.lse[head * a.tokens_q + token] * kLog2E, c = a.scale * kLog2E;
+  float lse = a.lse[head * a.tokens_q + token] * kLog2E;
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(lse));  // (see settle)
+#endif
+  const float c = a.scale * kLog2E;
   const int32_t lim = keys_of(a, w, i);
   v16f acc[H::kTiles];
 #pragma unroll
@@ -94,28 +98,15 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
   const int32_t most =
       uniform_i32(w.first + 32 * wave < w.rows ? keys_of(a, w, token_of(w.first + 32 * wave + 31)) : 0);
   const int32_t end = uniform_i32(keys_of(a, w, token_of(w.first + kBlock - 1)));
-  const uint32_t ldk = static_cast<uint32_t>(a.k.ld_token) * 2, ldv = static_cast<uint32_t>(a.v.ld_token) * 2;
-  const uint16_t* const kp = a.k.p + kvh * a.k.ld_head;
-  const uint16_t* const vp = a.v.p + kvh * a.v.ld_head;
-  const auto load = [&](int32_t kb, int slot) {
-    const int64_t t0 = static_cast<int64_t>(w.k0) + kb;
-    const rsrc_t rk = make_rsrc(kp + t0 * a.k.ld_token, -1), rv = make_rsrc(vp + t0 * a.v.ld_token, -1);
-    const int last = w.lk - 1 - kb;
-#pragma unroll
-    for (int n = 0; n < kLoads; ++n) {
-      const int r = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
-      const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
-      const uint32_t row = static_cast<uint32_t>(min(r, last));
-      uint8_t* const p = lds + slot * 2 * kTile + (wave * kLoads + n) * 1024;
-      dma16(rk, p, row * ldk + unit * 16);
-      dma16(rv, p + kTile, row * ldv + unit * 16);
-    }
-  };
-  if (end > 0) load(0, 0);
+  const KeyLoader<DP, kKeys, 4> keys(a, w, kvh, wave);
+  const uint32_t base = lds_offset(lds);
+  if (end > 0) keys.load(0, base, wave);
+  settle(q);
+  settle(dout);
   int slot = 0;
   for (int32_t kb = 0; kb < end; kb += kKeys) {
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    if (kb + kKeys < end) load(kb + kKeys, slot ^ 1);
+    wait_dma<0>();
+    if (kb + kKeys < end) keys.load(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
     uint8_t* const k = lds + slot * 2 * kTile;
     const uint8_t* const v = k + kTile;
     if (kb < most) {
@@ -184,6 +175,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionBwdArgs 
   const int64_t head0 = static_cast<int64_t>(kvh) * a.group;
   const rsrc_t rl = make_rsrc(a.lse + head0 * a.tokens_q + w.q0, -1);
   const rsrc_t rd = make_rsrc(a.delta + head0 * a.tokens_q + w.q0, -1);
+  const uint32_t base = lds_offset(lds);
   const uint32_t magic = 0xffffffffu / static_cast<uint32_t>(a.group) + 1;  // (0: a group of one)
   const auto load = [&](int32_t r0, int slot) {
     const int32_t t0 = uniform_i32(r0 / a.group);
@@ -203,23 +195,23 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionBwdArgs 
       const int r = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
       const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
       split(r, tk, g);
-      uint8_t* const p = lds + slot * kSlot + (wave * kLoads + n) * 1024;
+      const uint32_t p = base + slot * kSlot + (wave * kLoads + n) * 1024;
       dma16(rq, p, tk * ldq + g * lhq + unit * 16);
       dma16(ro, p + kTile, tk * ldo + g * lho + unit * 16);
     }
     if (wave < 2) {  // (lanes 32 and up repeat the rows, behind them)
       split(lane & 31, tk, g);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          wave == 0 ? rl : rd,
-          (__attribute__((address_space(3))) void*)(lds + slot * kSlot + 2 * kTile + wave * 256), 4,
-          (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4, 0, 0, 0);
+      dma4(wave == 0 ? rl : rd, base + slot * kSlot + 2 * kTile + wave * 256,
+           (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4);
     }
   };
   const float c = a.scale * kLog2E;
   if (begin < w.rows) load(begin, 0);
+  settle(k);
+  settle(v);
   int slot = 0;
   for (int32_t r0 = begin; r0 < w.rows; r0 += kRows) {
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    wait_dma<0>();
     if (r0 + kRows < w.rows) load(r0 + kRows, slot ^ 1);
     uint8_t* const q = lds + slot * kSlot;
     uint8_t* const dout = q + kTile;
