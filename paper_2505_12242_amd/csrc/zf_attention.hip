@@ -31,7 +31,7 @@ struct Rows {
 // One tile of keys, from key kb of the sequence on.  mask: some row sees only
 // some of them.
 template <int DP>
-__device__ __forceinline__ void tile_step(Rows<DP>& w, const uint8_t* k, uint8_t* v, int32_t kb,
+__device__ __forceinline__ void tile_step(Rows<DP>& w, uint32_t k, uint32_t v, int32_t kb,
                                           bool mask, float c) {
   typedef Heads<DP> H;
   const int half = threadIdx.x >> 5 & 1;
@@ -130,16 +130,15 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
   }
 
   const KeyLoader<DP, kKeys, 4> keys(a, w, kvh, wave);
-  const uint32_t base = lds_offset(lds);
+  const uint32_t base = lds_offset(lds), rows = H::lane_rows(), columns = H::lane_columns();
   if (begin < end) keys.load(begin, base, wave);
   settle(x.q);
   int slot = 0;
   for (int32_t kb = begin; kb < end; kb += kKeys) {
     wait_dma<0>();
     if (kb + kKeys < end) keys.load(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
-    const uint8_t* const k = lds + slot * 2 * kTile;
-    uint8_t* const v = lds + slot * 2 * kTile + kTile;
-    if (kb < most) tile_step<DP>(x, k, v, kb, kb + kKeys > least, a.scale * kLog2E);
+    const uint32_t at = base + slot * 2 * kTile;
+    if (kb < most) tile_step<DP>(x, at + rows, at + kTile + columns, kb, kb + kKeys > least, a.scale * kLog2E);
     slot ^= 1;
   }
 

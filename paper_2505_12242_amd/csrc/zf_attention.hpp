@@ -44,27 +44,30 @@ struct Heads {
   static __device__ __forceinline__ int swizzle(int r) {
     return kUnits == 16 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
   }
-  static __device__ __forceinline__ int at(int r, int unit) {
-    return r * kPitch + ((unit ^ swizzle(r)) << 4);
-  }
 
-  // Chunk c of rows r0 .. r0 + 31 (r0 a multiple of 16), a row a lane.
-  static __device__ __forceinline__ v8b frag(const uint8_t* lds, int r0, int c) {
-    const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const v8b*>(lds + r0 * kPitch +
-                                         at(lane & 31, 2 * c + (lane >> 5)));
+  // The lane's part of frag's and frag_t's addresses: what chunk, tile and row add
+  // are exclusive ors and sums of constants, so that a slot's start is added once.
+  static __device__ __forceinline__ uint32_t lane_rows() {
+    const int lane = threadIdx.x & 63, r = lane & 31;
+    return r * kPitch + (((lane >> 5) ^ swizzle(r)) << 4);
+  }
+  static __device__ __forceinline__ uint32_t lane_columns() {
+    const int lane = threadIdx.x & 63, i = lane & 15, r = 4 * (lane >> 5) + (i >> 2);
+    return r * kPitch + ((((lane >> 3 & 2) | (i >> 1 & 1)) ^ swizzle(r)) << 4) + 8 * (i & 1);
+  }
+  // Chunk c of rows r0 .. r0 + 31 (r0 a multiple of 16), a row a lane; `at`: byte of
+  // the tile in LDS plus lane_rows().
+  static __device__ __forceinline__ v8b frag(uint32_t at, int r0, int c) {
+    return *(const __attribute__((address_space(3))) v8b*)((at ^ (c << 5)) + r0 * kPitch);
   }
   // Columns 32 t .. 32 t + 31, a column a lane, of rows r0 .. r0 + 15 (r0 a
-  // multiple of 16) in the order above.
-  static __device__ __forceinline__ v8b frag_t(uint8_t* lds, int r0, int t) {
-    const int lane = threadIdx.x & 63, i = lane & 15;
-    const int row = 4 * (lane >> 5) + (i >> 2), unit = 4 * t + (lane >> 3 & 2) + (i >> 1 & 1);
+  // multiple of 16) in the order above; `at`: with lane_columns().
+  static __device__ __forceinline__ v8b frag_t(uint32_t at, int r0, int t) {
     v4s x[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) v4s*)(lds + r0 * kPitch + at(8 * e + row, unit) +
-                                                   8 * (i & 1)));
+      x[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(
+          (at ^ (t << 6 | e << 5)) + (r0 + 8 * e) * kPitch));
     return __builtin_bit_cast(
         v8b, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
       uniform_i32(w.first + 32 * wave < w.rows ? keys_of(a, w, token_of(w.first + 32 * wave + 31)) : 0);
   const int32_t end = uniform_i32(keys_of(a, w, token_of(w.first + kBlock - 1)));
   const KeyLoader<DP, kKeys, 4> keys(a, w, kvh, wave);
-  const uint32_t base = lds_offset(lds);
+  const uint32_t base = lds_offset(lds), rows = H::lane_rows(), columns = H::lane_columns();
   if (end > 0) keys.load(0, base, wave);
   settle(q);
   settle(dout);
@@ -107,8 +107,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
   for (int32_t kb = 0; kb < end; kb += kKeys) {
     wait_dma<0>();
     if (kb + kKeys < end) keys.load(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
-    uint8_t* const k = lds + slot * 2 * kTile;
-    const uint8_t* const v = k + kTile;
+    const uint32_t at = base + slot * 2 * kTile;
+    const uint32_t k = at + rows, kt = at + columns, v = at + kTile + rows;
     if (kb < most) {
       const bool mask = kb + kKeys > least;
 #pragma unroll
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
           const v8b ds = pack8(s, j);
 #pragma unroll
           for (int u = 0; u < H::kTiles; ++u)
-            acc[u] = mma(H::frag_t(k, 32 * t + 16 * j, u), ds, acc[u]);
+            acc[u] = mma(H::frag_t(kt, 32 * t + 16 * j, u), ds, acc[u]);
         }
       }
     }
@@ -142,11 +142,12 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
 }
 
 template <int DP>
-__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionBwdArgs a) {
+__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs a) {
   typedef Heads<DP> H;
   constexpr int kTile = kRows * H::kPitch, kLoads = kRows / H::kPer / 4;
-  constexpr int kSlot = 2 * kTile + 512;              // q, dout, lse and delta of the rows
-  __shared__ __align__(1024) uint8_t lds[2 * kSlot];
+  // q, dout, lse and delta of a tile's rows (these twice), and so many tiles at once
+  constexpr int kSlot = 2 * kTile + 1024, kSlots = 4, kTileLoads = 2 * kLoads + 1;
+  __shared__ __align__(1024) uint8_t lds[kSlots * kSlot];
   const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6), half = lane >> 5;
   const int32_t kvh = blockIdx.x % a.kv_heads;
   Sequence w;
@@ -199,29 +200,34 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionBwdArgs 
       dma16(rq, p, tk * ldq + g * lhq + unit * 16);
       dma16(ro, p + kTile, tk * ldo + g * lho + unit * 16);
     }
-    if (wave < 2) {  // (lanes 32 and up repeat the rows, behind them)
-      split(lane & 31, tk, g);
-      dma4(wave == 0 ? rl : rd, base + slot * kSlot + 2 * kTile + wave * 256,
-           (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4);
-    }
+    // (lanes 32 and up repeat the rows, behind them; waves 2 and 3 the first two)
+    split(lane & 31, tk, g);
+    dma4(wave & 1 ? rd : rl, base + slot * kSlot + 2 * kTile + wave * 256,
+         (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4);
   };
   const float c = a.scale * kLog2E;
-  if (begin < w.rows) load(begin, 0);
+  // tiles past the last repeat it, so that as many loads are always in flight
+  const int32_t last_tile = (w.rows - 1) / kRows * kRows;
+  if (begin < w.rows)
+#pragma unroll
+    for (int n = 0; n + 1 < kSlots; ++n) load(min(begin + n * kRows, last_tile), n);
   settle(k);
   settle(v);
+  const uint32_t lane_r = base + H::lane_rows(), lane_c = base + H::lane_columns();
   int slot = 0;
   for (int32_t r0 = begin; r0 < w.rows; r0 += kRows) {
-    wait_dma<0>();
-    if (r0 + kRows < w.rows) load(r0 + kRows, slot ^ 1);
-    uint8_t* const q = lds + slot * kSlot;
-    uint8_t* const dout = q + kTile;
-    const float* const stats = reinterpret_cast<const float*>(q + 2 * kTile);
+    wait_dma<(kSlots - 2) * kTileLoads>();
+    load(min(r0 + (kSlots - 1) * kRows, last_tile), (slot + kSlots - 1) % kSlots);
+    const uint32_t q = lane_r + slot * kSlot, qt = lane_c + slot * kSlot;
+    const uint32_t dout = q + kTile, dout_t = qt + kTile;
+    const float* const stats = reinterpret_cast<const float*>(lds + slot * kSlot + 2 * kTile);
     if (r0 + kRows > least) {
       v16f s = zero16(), dp = zero16();
 #pragma unroll
       for (int j = 0; j < H::kChunks; ++j) s = mma(H::frag(q, 0, j), k[j], s);
 #pragma unroll
       for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(dout, 0, j), v[j], dp);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int at = 8 * g + 4 * half;
@@ -241,17 +247,19 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(AttentionBwdArgs 
           if (row < from || row >= w.rows) s[r] = dp[r] = 0.0f;
         }
       }
+      const v8b p[2] = {pack8(s, 0), pack8(s, 1)}, ds[2] = {pack8(dp, 0), pack8(dp, 1)};
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const v8b p = pack8(s, j), ds = pack8(dp, j);
 #pragma unroll
-        for (int t = 0; t < H::kTiles; ++t) dv[t] = mma(H::frag_t(dout, 16 * j, t), p, dv[t]);
+        for (int t = 0; t < H::kTiles; ++t) dv[t] = mma(H::frag_t(dout_t, 16 * j, t), p[j], dv[t]);
 #pragma unroll
-        for (int t = 0; t < H::kTiles; ++t) dk[t] = mma(H::frag_t(q, 16 * j, t), ds, dk[t]);
+        for (int t = 0; t < H::kTiles; ++t) dk[t] = mma(H::frag_t(qt, 16 * j, t), ds[j], dk[t]);
       }
     }
-    slot ^= 1;
+    slot = (slot + 1) % kSlots;
   }
+  wait_dma<0>();  // (nothing lands in LDS once the block has ended)
   if (valid) {
     store_vector<DP>(a.dk.p + token * a.dk.ld_token + kvh * a.dk.ld_head, a.dim, dk, a.scale);
     store_vector<DP>(a.dv.p + token * a.dv.ld_token + kvh * a.dv.ld_head, a.dim, dv, 1.0f);
