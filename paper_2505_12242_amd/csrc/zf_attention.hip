@@ -79,10 +79,12 @@ __device__ __forceinline__ void tile_step(Rows<DP>& w, uint32_t k, uint32_t v, i
     p[2 * t] = pack8(s[t], 0);
     p[2 * t + 1] = pack8(s[t], 1);
   }
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int t = 0; t < H::kTiles; ++t)
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w.o[t] = mma(H::frag_t(v, 16 * j, t), p[j], w.o[t]);
+    for (int t = 0; t < H::kTiles; ++t) w.o[t] = mma(H::frag_t(v, 16 * j, t), p[j], w.o[t]);
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int DP, bool SPLIT>

@@ -228,6 +228,12 @@ __device__ __forceinline__ void wait_dma() {
   asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// The same without the other waves.
+template <int N>
+__device__ __forceinline__ void wait_own_dma() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 // Loads tiles of N keys of k and v: the wave's part of each (`waves` of them load
 // together), rows past the last key repeating it, units past the head's width
 // the last one (the other operand is zero there, or the result not stored).
@@ -294,6 +300,7 @@ struct AttentionBwdArgs {
   int64_t tokens_q, tokens_k;
   int32_t sequences, heads, kv_heads, group, dim, causal;
   int32_t tiles, key_tiles;
+  int32_t narrow;  // blocks of 32 keys, not 128
   float scale;
 };
 size_t attention_backward_workspace(const AttentionBwdArgs& a);

@@ -37,20 +37,35 @@ __device__ __forceinline__ void load_vector(const uint16_t* p, int dim, v8b (&x)
   }
 }
 
-// A gradient's vector, along the lane's registers of a result.
+// Tells the compiler to issue `reads` LDS reads and `products` products of the
+// region evenly, the reads `ahead` in front.
+template <int READS, int PRODUCTS, int AHEAD, int I = 0>
+__device__ __forceinline__ void reads_ahead() {
+  if constexpr (I == 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+  if constexpr (I < PRODUCTS) {
+    constexpr int kRest = READS - AHEAD;
+    constexpr int kReads = (I + 1) * kRest / PRODUCTS - I * kRest / PRODUCTS;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+    reads_ahead<READS, PRODUCTS, AHEAD, I + 1>();
+  }
+}
+
+// 32 elements (tile t) of a gradient's vector, along the lane's registers of a result.
+__device__ __forceinline__ void store_tile(uint16_t* p, int dim, int t, const v16f& x, float scale) {
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int d = 32 * t + 8 * g + 4 * (threadIdx.x >> 5 & 1);
+    if (d < dim)
+      *reinterpret_cast<u32x2*>(p + d) = u32x2{pack_bf16(x[4 * g] * scale, x[4 * g + 1] * scale),
+                                               pack_bf16(x[4 * g + 2] * scale, x[4 * g + 3] * scale)};
+  }
+}
 template <int DP>
 __device__ __forceinline__ void store_vector(uint16_t* p, int dim, const v16f (&x)[DP / 32],
                                              float scale) {
 #pragma unroll
-  for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d = 32 * t + 8 * g + 4 * (threadIdx.x >> 5 & 1);
-      if (d < dim)
-        *reinterpret_cast<u32x2*>(p + d) =
-            u32x2{pack_bf16(x[t][4 * g] * scale, x[t][4 * g + 1] * scale),
-                  pack_bf16(x[t][4 * g + 2] * scale, x[t][4 * g + 3] * scale)};
-    }
+  for (int t = 0; t < DP / 32; ++t) store_tile(p, dim, t, x[t], scale);
 }
 
 template <int DP>
@@ -141,23 +156,57 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
     store_vector<DP>(a.dq.p + token * a.dq.ld_token + head * a.dq.ld_head, a.dim, acc, a.scale);
 }
 
-template <int DP>
+// 32 WK keys a block, of which a wave keeps 32: k in registers, v in LDS.  WK 4:
+// the block's waves share each tile of rows.  WK 1: they have the same keys, and
+// every fourth tile of rows each (loaded by the wave for itself); their sums are
+// added in LDS, in the waves' order.
+// (LDS of the launch's own size: told that one block fills a CU's LDS, the compiler
+// takes twice the registers and copies sums between their two halves, 224 copies a
+// tile of rows.)
+template <int DP, int WK>
+struct Shared {
+  typedef Heads<DP> H;
+  static constexpr int kTile = kRows * H::kPitch;
+  static constexpr int kSlot = 2 * kTile + 1024;  // q, dout, lse and delta (256 bytes a wave)
+  static constexpr int kOwn = 2 * kSlot;          // of the waves that share tiles
+  static constexpr int kValues = 4 / WK * kOwn;   // the block's v
+  static constexpr int kAll = kValues + 32 * WK * H::kPitch;
+  static constexpr int kSums = WK == 4 ? 0 : 4 * 2 * H::kTiles * 4096;
+  static constexpr int kBytes = kAll > kSums ? kAll : kSums;
+};
+template <int DP, int WK>
 __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs a) {
   typedef Heads<DP> H;
-  constexpr int kTile = kRows * H::kPitch, kLoads = kRows / H::kPer / 4;
-  // q, dout, lse and delta of a tile's rows (these twice), and so many tiles at once
-  constexpr int kSlot = 2 * kTile + 1024, kSlots = 4, kTileLoads = 2 * kLoads + 1;
-  __shared__ __align__(1024) uint8_t lds[kSlots * kSlot];
+  typedef Shared<DP, WK> S;
+  constexpr int kTile = S::kTile, kSlot = S::kSlot, kOwn = S::kOwn, kValues = S::kValues;
+  constexpr int kLoads = kRows / H::kPer / WK;
+  constexpr int kStep = 4 / WK * kRows;  // from a wave's tile to its next
+  extern __shared__ __align__(1024) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6), half = lane >> 5;
+  const int part = WK == 4 ? wave : 0;     // of the block's keys
+  const int loader = WK == 4 ? wave : 0, own = WK == 4 ? 0 : wave;
   const int32_t kvh = blockIdx.x % a.kv_heads;
   Sequence w;
-  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, kLg, w)) return;
-  const int32_t key = w.first + 32 * wave + (lane & 31);
+  if (!find_tile<true>(a, blockIdx.x / a.kv_heads, WK == 4 ? kLg : 5, w)) return;
+  const int32_t key0 = w.first + 32 * part, key = key0 + (lane & 31);
   const bool valid = key < w.lk;
   const int64_t token = w.k0 + min(key, w.lk - 1);
-  v8b k[H::kChunks], v[H::kChunks];
+  const uint32_t base = lds_offset(lds);
+  v8b k[H::kChunks];
   load_vector<DP>(a.k.p + token * a.k.ld_token + kvh * a.k.ld_head, a.dim, k);
-  load_vector<DP>(a.v.p + token * a.v.ld_token + kvh * a.v.ld_head, a.dim, v);
+  {
+    const rsrc_t rv = make_rsrc(
+        a.v.p + (static_cast<int64_t>(w.k0) + w.first) * a.v.ld_token + kvh * a.v.ld_head, -1);
+    constexpr int kN = 32 * WK / H::kPer / 4;
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      const int r = (wave * kN + n) * H::kPer + lane / H::kUnits;
+      const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
+      dma16(rv, base + kValues + (wave * kN + n) * 1024,
+            static_cast<uint32_t>(min(r, w.lk - 1 - w.first)) *
+                    (static_cast<uint32_t>(a.v.ld_token) * 2) + unit * 16);
+    }
+  }
   v16f dk[H::kTiles], dv[H::kTiles];
 #pragma unroll
   for (int t = 0; t < H::kTiles; ++t) dk[t] = dv[t] = zero16();
@@ -166,17 +215,15 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
     return a.causal ? max(key - (w.lk - w.lq), 0) * a.group : 0;
   };
   const int32_t from = first_row(min(key, w.lk - 1));
-  const int32_t most = uniform_i32(first_row(min(w.first + 32 * wave + 31, w.lk - 1)));
-  const int32_t least = uniform_i32(
-      w.first + 32 * wave < w.lk ? first_row(w.first + 32 * wave) : w.rows);
-  const int32_t begin = uniform_i32(first_row(w.first)) / kRows * kRows;
+  const int32_t most = uniform_i32(first_row(min(key0 + 31, w.lk - 1)));
+  const int32_t least = uniform_i32(key0 < w.lk ? first_row(key0) : w.rows);
+  const int32_t begin = uniform_i32(first_row(w.first)) / kRows * kRows + own * kRows;
 
   const uint32_t ldq = static_cast<uint32_t>(a.q.ld_token) * 2, ldo = static_cast<uint32_t>(a.dout.ld_token) * 2;
   const uint32_t lhq = static_cast<uint32_t>(a.q.ld_head) * 2, lho = static_cast<uint32_t>(a.dout.ld_head) * 2;
   const int64_t head0 = static_cast<int64_t>(kvh) * a.group;
   const rsrc_t rl = make_rsrc(a.lse + head0 * a.tokens_q + w.q0, -1);
   const rsrc_t rd = make_rsrc(a.delta + head0 * a.tokens_q + w.q0, -1);
-  const uint32_t base = lds_offset(lds);
   const uint32_t magic = 0xffffffffu / static_cast<uint32_t>(a.group) + 1;  // (0: a group of one)
   const auto load = [&](int32_t r0, int slot) {
     const int32_t t0 = uniform_i32(r0 / a.group);
@@ -185,6 +232,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
     const rsrc_t rq = make_rsrc(a.q.p + tok * a.q.ld_token + head0 * a.q.ld_head, -1);
     const rsrc_t ro = make_rsrc(a.dout.p + tok * a.dout.ld_token + head0 * a.dout.ld_head, -1);
     const int last = w.rows - 1 - r0;
+    const uint32_t to = base + own * kOwn + slot * kSlot;
     const auto split = [&](int r, uint32_t& tok, uint32_t& g) {  // row r0 + r
       const uint32_t x = in + static_cast<uint32_t>(min(r, last));
       tok = magic ? __umulhi(x, magic) : x;
@@ -193,41 +241,56 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
     uint32_t tk, g;
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
-      const int r = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
+      const int r = (loader * kLoads + n) * H::kPer + lane / H::kUnits;
       const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
       split(r, tk, g);
-      const uint32_t p = base + slot * kSlot + (wave * kLoads + n) * 1024;
+      const uint32_t p = to + (loader * kLoads + n) * 1024;
       dma16(rq, p, tk * ldq + g * lhq + unit * 16);
       dma16(ro, p + kTile, tk * ldo + g * lho + unit * 16);
     }
     // (lanes 32 and up repeat the rows, behind them; waves 2 and 3 the first two)
     split(lane & 31, tk, g);
-    dma4(wave & 1 ? rd : rl, base + slot * kSlot + 2 * kTile + wave * 256,
-         (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4);
+    const uint32_t at = (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4;
+    if constexpr (WK == 4) {
+      dma4(wave & 1 ? rd : rl, to + 2 * kTile + wave * 256, at);
+    } else {
+      dma4(rl, to + 2 * kTile, at);
+      dma4(rd, to + 2 * kTile + 256, at);
+    }
   };
   const float c = a.scale * kLog2E;
-  // tiles past the last repeat it, so that as many loads are always in flight
-  const int32_t last_tile = (w.rows - 1) / kRows * kRows;
-  if (begin < w.rows)
-#pragma unroll
-    for (int n = 0; n + 1 < kSlots; ++n) load(min(begin + n * kRows, last_tile), n);
+  if (begin < w.rows) load(begin, 0);
   settle(k);
-  settle(v);
   const uint32_t lane_r = base + H::lane_rows(), lane_c = base + H::lane_columns();
+  if (WK != 4 || a.dim < DP) wait_dma<0>();  // (every wave's part of v)
+  if (a.dim < DP) {  // dout's units past the head's width hold anything: v's are zeros
+    const int first = a.dim / 8, n = DP / 8 - first;
+    for (int i = threadIdx.x; i < 32 * WK * n; i += 256) {
+      const int r = i / n, unit = first + i - r * n;
+      *reinterpret_cast<u32x4*>(lds + kValues + r * H::kPitch + ((unit ^ H::swizzle(r)) << 4)) =
+          u32x4{0, 0, 0, 0};
+    }
+    __syncthreads();
+  }
   int slot = 0;
-  for (int32_t r0 = begin; r0 < w.rows; r0 += kRows) {
-    wait_dma<(kSlots - 2) * kTileLoads>();
-    load(min(r0 + (kSlots - 1) * kRows, last_tile), (slot + kSlots - 1) % kSlots);
-    const uint32_t q = lane_r + slot * kSlot, qt = lane_c + slot * kSlot;
-    const uint32_t dout = q + kTile, dout_t = qt + kTile;
-    const float* const stats = reinterpret_cast<const float*>(lds + slot * kSlot + 2 * kTile);
+  for (int32_t r0 = begin; r0 < w.rows; r0 += kStep) {
+    if (WK == 4) wait_dma<0>();
+    else wait_own_dma<0>();
+    if (r0 + kStep < w.rows) load(r0 + kStep, slot ^ 1);
+    const uint32_t q = lane_r + own * kOwn + slot * kSlot, qt = lane_c + own * kOwn + slot * kSlot;
+    const uint32_t dout = q + kTile, dout_t = qt + kTile, v = lane_r + kValues + part * 32 * H::kPitch;
+    const float* const stats =
+        reinterpret_cast<const float*>(lds + own * kOwn + slot * kSlot + 2 * kTile);
     if (r0 + kRows > least) {
       v16f s = zero16(), dp = zero16();
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int j = 0; j < H::kChunks; ++j) s = mma(H::frag(q, 0, j), k[j], s);
 #pragma unroll
-      for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(dout, 0, j), v[j], dp);
+      for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(dout, 0, j), H::frag(v, 0, j), dp);
+      reads_ahead<3 * H::kChunks, 2 * H::kChunks, 5>();
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int at = 8 * g + 4 * half;
@@ -249,31 +312,69 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
       }
       const v8b p[2] = {pack8(s, 0), pack8(s, 1)}, ds[2] = {pack8(dp, 0), pack8(dp, 1)};
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
-        for (int t = 0; t < H::kTiles; ++t) dv[t] = mma(H::frag_t(dout_t, 16 * j, t), p[j], dv[t]);
-#pragma unroll
-        for (int t = 0; t < H::kTiles; ++t) dk[t] = mma(H::frag_t(qt, 16 * j, t), ds[j], dk[t]);
+        for (int t = 0; t < H::kTiles; ++t) {
+          dv[t] = mma(H::frag_t(dout_t, 16 * j, t), p[j], dv[t]);
+          dk[t] = mma(H::frag_t(qt, 16 * j, t), ds[j], dk[t]);
+        }
       }
+      reads_ahead<8 * H::kTiles, 4 * H::kTiles, 6>();
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(0);
     }
-    slot = (slot + 1) % kSlots;
+    slot ^= 1;
   }
-  wait_dma<0>();  // (nothing lands in LDS once the block has ended)
-  if (valid) {
-    store_vector<DP>(a.dk.p + token * a.dk.ld_token + kvh * a.dk.ld_head, a.dim, dk, a.scale);
-    store_vector<DP>(a.dv.p + token * a.dv.ld_token + kvh * a.dv.ld_head, a.dim, dv, 1.0f);
+  uint16_t* const to_k = a.dk.p + token * a.dk.ld_token + kvh * a.dk.ld_head;
+  uint16_t* const to_v = a.dv.p + token * a.dv.ld_token + kvh * a.dv.ld_head;
+  if constexpr (WK == 4) {
+    if (valid) {
+      store_vector<DP>(to_k, a.dim, dk, a.scale);
+      store_vector<DP>(to_v, a.dim, dv, 1.0f);
+    }
+  } else {
+    // (all loads have landed: a wave waits for its last tile's)
+    float* const sums = reinterpret_cast<float*>(lds);
+    const auto place = [&](int wave, int u, int r) {
+      return sums + ((wave * 2 * H::kTiles + u) * 16 + r) * 64 + lane;
+    };
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < H::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        *place(wave, t, r) = dk[t][r];
+        *place(wave, H::kTiles + t, r) = dv[t][r];
+      }
+    __syncthreads();
+    for (int u = wave; u < 2 * H::kTiles; u += 4) {
+      v16f x;
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        x[r] = ((*place(0, u, r) + *place(1, u, r)) + *place(2, u, r)) + *place(3, u, r);
+      if (!valid) continue;
+      if (u < H::kTiles) store_tile(to_k, a.dim, u, x, a.scale);
+      else store_tile(to_v, a.dim, u - H::kTiles, x, 1.0f);
+    }
   }
 }
+
+// Blocks of 128 keys that fill the chip's 512 places, below which blocks of 32 keys
+// are taken.
+constexpr int64_t kFewBlocks = 512;
 
 template <int DP>
 void launch(const AttentionBwdArgs& a, hipStream_t s) {
   if (a.tokens_q > 0)
     hipLaunchKernelGGL((attention_dq_kernel<DP>), dim3(static_cast<uint32_t>(a.tiles) * a.kv_heads),
                        dim3(256), 0, s, a);
-  if (a.tokens_k > 0)
-    hipLaunchKernelGGL((attention_dkv_kernel<DP>),
-                       dim3(static_cast<uint32_t>(a.key_tiles) * a.kv_heads), dim3(256), 0, s, a);
+  if (a.tokens_k == 0) return;
+  const dim3 grid(static_cast<uint32_t>(a.key_tiles) * a.kv_heads);
+  constexpr int kNarrow = Shared<DP, 1>::kBytes, kWide = Shared<DP, 4>::kBytes;
+  if (a.narrow) hipLaunchKernelGGL((attention_dkv_kernel<DP, 1>), grid, dim3(256), kNarrow, s, a);
+  else hipLaunchKernelGGL((attention_dkv_kernel<DP, 4>), grid, dim3(256), kWide, s, a);
 }
 
 }  // namespace
@@ -286,7 +387,8 @@ hipError_t launch_attention_backward(AttentionBwdArgs a, void* ws, hipStream_t s
   (void)hipGetLastError();
   a.delta = static_cast<float*>(ws);
   a.tiles = static_cast<int32_t>((a.tokens_q * a.group >> kLg) + a.sequences);
-  a.key_tiles = static_cast<int32_t>((a.tokens_k >> kLg) + a.sequences);
+  a.narrow = ((a.tokens_k >> kLg) + a.sequences) * a.kv_heads < kFewBlocks;
+  a.key_tiles = static_cast<int32_t>((a.tokens_k >> (a.narrow ? 5 : kLg)) + a.sequences);
   if (a.dim <= 64) launch<64>(a, s);
   else if (a.dim <= 96) launch<96>(a, s);
   else launch<128>(a, s);
