@@ -252,7 +252,7 @@ typedef struct zf_heads {
  * key head h / (heads / kv_heads).
  * dim: a multiple of 8 up to 128.  heads: a multiple of kv_heads, up to 2^16.
  * scale: finite, > 0.  tokens < 2^30, max(tokens_q * heads, tokens_k * kv_heads)
- * / 16 + sequences * kv_heads < 2^24. */
+ * / 16 + sequences * kv_heads < 2^23. */
 typedef struct zf_attention {
   int64_t tokens_q;
   int64_t tokens_k;

@@ -300,7 +300,6 @@ struct AttentionBwdArgs {
   int64_t tokens_q, tokens_k;
   int32_t sequences, heads, kv_heads, group, dim, causal;
   int32_t tiles, key_tiles;
-  int32_t narrow;  // blocks of 32 keys, not 128
   float scale;
 };
 size_t attention_backward_workspace(const AttentionBwdArgs& a);

@@ -156,35 +156,34 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
     store_vector<DP>(a.dq.p + token * a.dq.ld_token + head * a.dq.ld_head, a.dim, acc, a.scale);
 }
 
-// 32 WK keys a block, of which a wave keeps 32: k in registers, v in LDS.  WK 4:
-// the block's waves share each tile of rows.  WK 1: they have the same keys, and
-// every fourth tile of rows each (loaded by the wave for itself); their sums are
-// added in LDS, in the waves' order.
+// 32 WK keys a block, of which a wave keeps 32: k in registers, v in LDS.  WR groups
+// of WK waves have the same keys and every WR-th tile of rows each, which the
+// group's waves load together and share; the groups' sums are added in LDS, in
+// their order.
 // (LDS of the launch's own size: told that one block fills a CU's LDS, the compiler
 // takes twice the registers and copies sums between their two halves, 224 copies a
 // tile of rows.)
-template <int DP, int WK>
+template <int DP, int WK, int WR>
 struct Shared {
   typedef Heads<DP> H;
   static constexpr int kTile = kRows * H::kPitch;
   static constexpr int kSlot = 2 * kTile + 1024;  // q, dout, lse and delta (256 bytes a wave)
-  static constexpr int kOwn = 2 * kSlot;          // of the waves that share tiles
-  static constexpr int kValues = 4 / WK * kOwn;   // the block's v
+  static constexpr int kOwn = 2 * kSlot;          // of a group
+  static constexpr int kValues = WR * kOwn;       // the block's v
   static constexpr int kAll = kValues + 32 * WK * H::kPitch;
-  static constexpr int kSums = WK == 4 ? 0 : 4 * 2 * H::kTiles * 4096;
+  static constexpr int kSums = (WR - 1) * WK * H::kTiles * 4096;
   static constexpr int kBytes = kAll > kSums ? kAll : kSums;
 };
-template <int DP, int WK>
-__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs a) {
+template <int DP, int WK, int WR>
+__global__ __launch_bounds__(64 * WK * WR, 2) void attention_dkv_kernel(AttentionBwdArgs a) {
   typedef Heads<DP> H;
-  typedef Shared<DP, WK> S;
+  typedef Shared<DP, WK, WR> S;
   constexpr int kTile = S::kTile, kSlot = S::kSlot, kOwn = S::kOwn, kValues = S::kValues;
   constexpr int kLoads = kRows / H::kPer / WK;
-  constexpr int kStep = 4 / WK * kRows;  // from a wave's tile to its next
+  constexpr int kStep = WR * kRows;  // from a group's tile to its next
   extern __shared__ __align__(1024) uint8_t lds[];
   const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6), half = lane >> 5;
-  const int part = WK == 4 ? wave : 0;     // of the block's keys
-  const int loader = WK == 4 ? wave : 0, own = WK == 4 ? 0 : wave;
+  const int part = wave % WK, own = wave / WK;  // of the block's keys, the group
   const int32_t kvh = blockIdx.x % a.kv_heads;
   Sequence w;
   if (!find_tile<true>(a, blockIdx.x / a.kv_heads, WK == 4 ? kLg : 5, w)) return;
@@ -197,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
   {
     const rsrc_t rv = make_rsrc(
         a.v.p + (static_cast<int64_t>(w.k0) + w.first) * a.v.ld_token + kvh * a.v.ld_head, -1);
-    constexpr int kN = 32 * WK / H::kPer / 4;
+    constexpr int kN = 32 / H::kPer / WR;
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
       const int r = (wave * kN + n) * H::kPer + lane / H::kUnits;
@@ -241,18 +240,18 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
     uint32_t tk, g;
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
-      const int r = (loader * kLoads + n) * H::kPer + lane / H::kUnits;
+      const int r = (part * kLoads + n) * H::kPer + lane / H::kUnits;
       const int unit = min((lane % H::kUnits) ^ H::swizzle(r), a.dim / 8 - 1);
       split(r, tk, g);
-      const uint32_t p = to + (loader * kLoads + n) * 1024;
+      const uint32_t p = to + (part * kLoads + n) * 1024;
       dma16(rq, p, tk * ldq + g * lhq + unit * 16);
       dma16(ro, p + kTile, tk * ldo + g * lho + unit * 16);
     }
-    // (lanes 32 and up repeat the rows, behind them; waves 2 and 3 the first two)
+    // (lanes 32 and up repeat the rows, behind them; parts 2 and 3 the first two)
     split(lane & 31, tk, g);
     const uint32_t at = (g * static_cast<uint32_t>(a.tokens_q) + static_cast<uint32_t>(t0) + tk) * 4;
     if constexpr (WK == 4) {
-      dma4(wave & 1 ? rd : rl, to + 2 * kTile + wave * 256, at);
+      dma4(part & 1 ? rd : rl, to + 2 * kTile + part * 256, at);
     } else {
       dma4(rl, to + 2 * kTile, at);
       dma4(rd, to + 2 * kTile + 256, at);
@@ -262,10 +261,10 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
   if (begin < w.rows) load(begin, 0);
   settle(k);
   const uint32_t lane_r = base + H::lane_rows(), lane_c = base + H::lane_columns();
-  if (WK != 4 || a.dim < DP) wait_dma<0>();  // (every wave's part of v)
+  if (WK == 1 || a.dim < DP) wait_dma<0>();  // (every wave's part of v)
   if (a.dim < DP) {  // dout's units past the head's width hold anything: v's are zeros
     const int first = a.dim / 8, n = DP / 8 - first;
-    for (int i = threadIdx.x; i < 32 * WK * n; i += 256) {
+    for (int i = threadIdx.x; i < 32 * WK * n; i += 64 * WK * WR) {
       const int r = i / n, unit = first + i - r * n;
       *reinterpret_cast<u32x4*>(lds + kValues + r * H::kPitch + ((unit ^ H::swizzle(r)) << 4)) =
           u32x4{0, 0, 0, 0};
@@ -273,15 +272,17 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
     __syncthreads();
   }
   int slot = 0;
-  for (int32_t r0 = begin; r0 < w.rows; r0 += kStep) {
-    if (WK == 4) wait_dma<0>();
-    else wait_own_dma<0>();
+  // (groups that share barriers walk as many tiles, the last one perhaps of none)
+  const int32_t end = WK == 1 ? w.rows : w.rows + own * kRows;
+  for (int32_t r0 = begin; r0 < end; r0 += kStep) {
+    if (WK == 1) wait_own_dma<0>();
+    else wait_dma<0>();
     if (r0 + kStep < w.rows) load(r0 + kStep, slot ^ 1);
     const uint32_t q = lane_r + own * kOwn + slot * kSlot, qt = lane_c + own * kOwn + slot * kSlot;
     const uint32_t dout = q + kTile, dout_t = qt + kTile, v = lane_r + kValues + part * 32 * H::kPitch;
     const float* const stats =
         reinterpret_cast<const float*>(lds + own * kOwn + slot * kSlot + 2 * kTile);
-    if (r0 + kRows > least) {
+    if (r0 + kRows > least && r0 < w.rows) {
       v16f s = zero16(), dp = zero16();
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -329,41 +330,58 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBwdArgs 
   }
   uint16_t* const to_k = a.dk.p + token * a.dk.ld_token + kvh * a.dk.ld_head;
   uint16_t* const to_v = a.dv.p + token * a.dv.ld_token + kvh * a.dv.ld_head;
-  if constexpr (WK == 4) {
-    if (valid) {
-      store_vector<DP>(to_k, a.dim, dk, a.scale);
-      store_vector<DP>(to_v, a.dim, dv, 1.0f);
-    }
-  } else {
-    // (all loads have landed: a wave waits for its last tile's)
-    float* const sums = reinterpret_cast<float*>(lds);
-    const auto place = [&](int wave, int u, int r) {
-      return sums + ((wave * 2 * H::kTiles + u) * 16 + r) * 64 + lane;
+  // (all loads have landed: a wave waits for its last tile's)
+  float* const sums = reinterpret_cast<float*>(lds);
+  const auto join = [&](v16f(&x)[H::kTiles]) {
+    const auto place = [&](int group, int t, int r) {
+      return sums + ((((group - 1) * WK + part) * H::kTiles + t) * 16 + r) * 64 + lane;
     };
     __syncthreads();
+    if (own > 0)
 #pragma unroll
-    for (int t = 0; t < H::kTiles; ++t)
+      for (int t = 0; t < H::kTiles; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        *place(wave, t, r) = dk[t][r];
-        *place(wave, H::kTiles + t, r) = dv[t][r];
-      }
+        for (int r = 0; r < 16; ++r) *place(own, t, r) = x[t][r];
     __syncthreads();
-    for (int u = wave; u < 2 * H::kTiles; u += 4) {
-      v16f x;
+    if (own == 0)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        x[r] = ((*place(0, u, r) + *place(1, u, r)) + *place(2, u, r)) + *place(3, u, r);
-      if (!valid) continue;
-      if (u < H::kTiles) store_tile(to_k, a.dim, u, x, a.scale);
-      else store_tile(to_v, a.dim, u - H::kTiles, x, 1.0f);
-    }
+      for (int g = 1; g < WR; ++g)
+#pragma unroll
+        for (int t = 0; t < H::kTiles; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x[t][r] += *place(g, t, r);
+  };
+  if (WR > 1) {
+    join(dk);
+    join(dv);
+  }
+  if (own == 0 && valid) {
+    store_vector<DP>(to_k, a.dim, dk, a.scale);
+    store_vector<DP>(to_v, a.dim, dv, 1.0f);
   }
 }
 
-// Blocks of 128 keys that fill the chip's 512 places, below which blocks of 32 keys
-// are taken.
-constexpr int64_t kFewBlocks = 512;
+// Forms by the number of blocks of 128 keys (of 512 that the chip holds at once).
+// Few: blocks of 32 keys, a wave's walk a quarter as long (5 sequences of some 500 x
+// 4 key heads 95 us, not 214; 4 x 1024 x 12 heads 60.8, two groups 63.5).  Causal, up
+// to two rounds: the first keys' blocks would be the last to end, so two groups of
+// waves share a walk (8192 x 8 key heads 1940 us, one group 2400; whole 485, not 466).
+// Else one group, without the second one's barriers (2 x 4096 x 32 heads 993, not 1046).
+enum { kNarrow, kTwoGroups, kWide };
+constexpr int64_t kFewBlocks = 448, kTwoRounds = 1024;
+int32_t form_of(const AttentionBwdArgs& a) {
+  const int64_t blocks = ((a.tokens_k >> kLg) + a.sequences) * a.kv_heads;
+  if (blocks < kFewBlocks) return kNarrow;
+  return a.causal && blocks < kTwoRounds ? kTwoGroups : kWide;
+}
+
+template <int DP, int WK, int WR>
+void launch_dkv(const AttentionBwdArgs& a, hipStream_t s) {
+  constexpr int kBytes = Shared<DP, WK, WR>::kBytes;
+  hipLaunchKernelGGL((attention_dkv_kernel<DP, WK, WR>),
+                     dim3(static_cast<uint32_t>(a.key_tiles) * a.kv_heads), dim3(64 * WK * WR),
+                     kBytes, s, a);
+}
 
 template <int DP>
 void launch(const AttentionBwdArgs& a, hipStream_t s) {
@@ -371,10 +389,10 @@ void launch(const AttentionBwdArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((attention_dq_kernel<DP>), dim3(static_cast<uint32_t>(a.tiles) * a.kv_heads),
                        dim3(256), 0, s, a);
   if (a.tokens_k == 0) return;
-  const dim3 grid(static_cast<uint32_t>(a.key_tiles) * a.kv_heads);
-  constexpr int kNarrow = Shared<DP, 1>::kBytes, kWide = Shared<DP, 4>::kBytes;
-  if (a.narrow) hipLaunchKernelGGL((attention_dkv_kernel<DP, 1>), grid, dim3(256), kNarrow, s, a);
-  else hipLaunchKernelGGL((attention_dkv_kernel<DP, 4>), grid, dim3(256), kWide, s, a);
+  const int32_t form = form_of(a);
+  if (form == kNarrow) launch_dkv<DP, 1, 4>(a, s);
+  else if (form == kTwoGroups) launch_dkv<DP, 4, 2>(a, s);
+  else launch_dkv<DP, 4, 1>(a, s);
 }
 
 }  // namespace
@@ -387,8 +405,8 @@ hipError_t launch_attention_backward(AttentionBwdArgs a, void* ws, hipStream_t s
   (void)hipGetLastError();
   a.delta = static_cast<float*>(ws);
   a.tiles = static_cast<int32_t>((a.tokens_q * a.group >> kLg) + a.sequences);
-  a.narrow = ((a.tokens_k >> kLg) + a.sequences) * a.kv_heads < kFewBlocks;
-  a.key_tiles = static_cast<int32_t>((a.tokens_k >> (a.narrow ? 5 : kLg)) + a.sequences);
+  a.key_tiles =
+      static_cast<int32_t>((a.tokens_k >> (form_of(a) == kNarrow ? 5 : kLg)) + a.sequences);
   if (a.dim <= 64) launch<64>(a, s);
   else if (a.dim <= 96) launch<96>(a, s);
   else launch<128>(a, s);

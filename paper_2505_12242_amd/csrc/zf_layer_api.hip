@@ -125,10 +125,10 @@ bool attention_ok(const zf_attention* a) {
   if ((a->seq_q == nullptr) != (a->seq_k == nullptr)) return false;
   if (a->seq_q == nullptr && (a->sequences != 1 || a->len_k != nullptr)) return false;
   if (!aligned(a->seq_q, 4) || !aligned(a->seq_k, 4) || !aligned(a->len_k, 4)) return false;
-  // rows and keys, of all heads, that a launch's blocks of 16 still reach (and
-  // that 32 bits count)
+  // rows and keys, of all heads, that a launch's blocks (of 512 threads) still
+  // reach, and that 32 bits count
   return (std::max(a->tokens_q * a->heads, a->tokens_k * a->kv_heads) / 16 +
-          static_cast<int64_t>(a->sequences) * a->kv_heads) < kGridLimit;
+          static_cast<int64_t>(a->sequences) * a->kv_heads) < kGridLimit / 2;
 }
 
 // Bytes from the first to past the last element.  `ok` is cleared where the
