@@ -28,63 +28,146 @@ struct Rows {
   int32_t lim;   // keys that the lane's row sees
 };
 
-// One tile of keys, from key kb of the sequence on.  mask: some row sees only
-// some of them.
-template <int DP>
-__device__ __forceinline__ void tile_step(Rows<DP>& w, uint32_t k, uint32_t v, int32_t kb,
-                                          bool mask, float c) {
+// One tile of KEYS keys, from key kb of the sequence on, its scores and its
+// values.  mask: some row sees only some of them.
+template <int DP, int KEYS>
+struct Tile {
   typedef Heads<DP> H;
-  const int half = threadIdx.x >> 5 & 1;
-  v16f s[2];
+  v16f s[KEYS / 32];
+  v8b p[KEYS / 16];
+
+  __device__ __forceinline__ void scores(const Rows<DP>& w, uint32_t k) {
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    s[t] = zero16();
+    for (int t = 0; t < KEYS / 32; ++t) {
+      s[t] = zero16();
 #pragma unroll
-    for (int j = 0; j < H::kChunks; ++j) s[t] = mma(H::frag(k, 32 * t, j), w.q[j], s[t]);
-  }
-  __builtin_amdgcn_sched_barrier(0);
-  if (mask) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (kb + 32 * t + reg_row(r) + 4 * half >= w.lim) s[t][r] = -INFINITY;
-  }
-  float top = -INFINITY;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-  top = fmaxf(top, other_half(top));
-  // (the first tile that a row sees anything of has m = -infinity)
-  if (__any(top * c > w.m * c + 8.0f)) {
-    const float m = fmaxf(w.m, top);
-    const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((w.m - m) * c);
-    w.m = m;
-    w.l *= f;
-#pragma unroll
-    for (int t = 0; t < H::kTiles; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) w.o[t][r] *= f;
-  }
-  const float mc = w.m == -INFINITY ? 0.0f : w.m * c;
-  v8b p[4];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c, -mc));
-      w.l += s[t][r];
+      for (int j = 0; j < H::kChunks; ++j) s[t] = mma(H::frag(k, 32 * t, j), w.q[j], s[t]);
     }
-    p[2 * t] = pack8(s[t], 0);
-    p[2 * t + 1] = pack8(s[t], 1);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  __builtin_amdgcn_sched_barrier(0);
+  __device__ __forceinline__ void weights(Rows<DP>& w, int32_t kb, bool mask, float c) {
+    if (mask) {
+      const int half = threadIdx.x >> 5 & 1;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+      for (int t = 0; t < KEYS / 32; ++t)
 #pragma unroll
-    for (int t = 0; t < H::kTiles; ++t) w.o[t] = mma(H::frag_t(v, 16 * j, t), p[j], w.o[t]);
-  __builtin_amdgcn_sched_barrier(0);
+        for (int r = 0; r < 16; ++r)
+          if (kb + 32 * t + reg_row(r) + 4 * half >= w.lim) s[t][r] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < KEYS / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+    top = fmaxf(top, other_half(top));
+    // (the first tile that a row sees anything of has m = -infinity)
+    if (__any(top * c > w.m * c + 8.0f)) {
+      const float m = fmaxf(w.m, top);
+      const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((w.m - m) * c);
+      w.m = m;
+      w.l *= f;
+#pragma unroll
+      for (int t = 0; t < H::kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w.o[t][r] *= f;
+    }
+    const float mc = w.m == -INFINITY ? 0.0f : w.m * c;
+#pragma unroll
+    for (int t = 0; t < KEYS / 32; ++t) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c, -mc));
+        w.l += s[t][r];
+      }
+      p[2 * t] = pack8(s[t], 0);
+      p[2 * t + 1] = pack8(s[t], 1);
+    }
+  }
+  __device__ __forceinline__ void values(Rows<DP>& w, uint32_t v) const {
+#pragma unroll
+    for (int j = 0; j < KEYS / 16; ++j)
+#pragma unroll
+      for (int t = 0; t < H::kTiles; ++t) w.o[t] = mma(H::frag_t(v, 16 * j, t), p[j], w.o[t]);
+  }
+};
+
+// The lane's row: row `row` of the sequence, or its last where there are fewer
+// (`valid`: it is the row itself).
+struct Place {
+  bool valid;
+  int32_t token;  // of the sequence
+  int64_t head;
+};
+__device__ __forceinline__ Place place_row(const AttentionArgs& a, const Sequence& w, int32_t kvh,
+                                           int32_t row) {
+  Place p;
+  p.valid = row < w.rows;
+  row = min(row, w.rows - 1);
+  p.token = row / a.group;
+  p.head = static_cast<int64_t>(kvh) * a.group + (row - p.token * a.group);
+  return p;
+}
+
+template <int DP>
+__device__ __forceinline__ void start_rows(const AttentionArgs& a, const Sequence& w,
+                                           const Place& at, Rows<DP>& x) {
+  typedef Heads<DP> H;
+  x.lim = keys_of(a, w, at.token);
+  x.m = -INFINITY;
+  x.l = 0.0f;
+  const uint16_t* const q = a.q.p + static_cast<int64_t>(w.q0 + at.token) * a.q.ld_token + at.head * a.q.ld_head;
+#pragma unroll
+  for (int c = 0; c < H::kChunks; ++c) {
+    const int e = 16 * c + 8 * (threadIdx.x >> 5 & 1);
+    u32x4 u = {0, 0, 0, 0};
+    if (e < a.dim) u = *reinterpret_cast<const u32x4*>(q + e);
+    x.q[c] = __builtin_bit_cast(v8b, u);
+  }
+#pragma unroll
+  for (int t = 0; t < H::kTiles; ++t) x.o[t] = zero16();
+}
+
+// 32 elements (tile t) of a row's result, `part` < 0: of out itself.
+__device__ __forceinline__ void store_out(const AttentionArgs& a, const Sequence& w, const Place& at,
+                                          int32_t part, int t, const v16f& o, float inv) {
+  const int64_t token = w.q0 + at.token;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int d = 32 * t + 8 * g + 4 * (threadIdx.x >> 5 & 1);
+    if (d >= a.dim) continue;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = o[4 * g + e] * inv;
+    if (part >= 0) {
+      const int64_t row = (part * static_cast<int64_t>(a.heads) + at.head) * a.tokens_q + token;
+      *reinterpret_cast<u32x4*>(a.part_out + row * a.dim + d) =
+          u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else {
+      *reinterpret_cast<u32x2*>(a.out + token * a.ld_out_token + at.head * a.ld_out_head + d) =
+          u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    }
+  }
+}
+// A row's 1 / sum and its lse, stored; zero and -infinity where it sees no key.
+__device__ __forceinline__ float finish_row(const AttentionArgs& a, const Sequence& w, const Place& at,
+                                            int32_t part, float m, float sum, bool store) {
+  const bool any = sum > 0.0f || sum != sum;
+  const float lse = any ? fmaf(m, a.scale, kLn2 * __log2f(sum)) : -INFINITY;
+  if (at.valid && store) {
+    const int64_t row = at.head * a.tokens_q + w.q0 + at.token;
+    if (part >= 0) a.part_lse[static_cast<int64_t>(part) * a.heads * a.tokens_q + row] = lse;
+    else if (a.lse != nullptr) a.lse[row] = lse;
+  }
+  return any ? 1.0f / sum : 0.0f;
+}
+
+// Keys of a piece of a sequence of lk keys, and how many pieces it has.
+__device__ __forceinline__ int32_t piece_of(const AttentionArgs& a, int32_t lk) {
+  return max(a.piece, ((lk + a.splits - 1) / a.splits + 127) / 128 * 128);
+}
+__device__ __forceinline__ int32_t pieces_of(const AttentionArgs& a, int32_t lk) {
+  const int32_t piece = piece_of(a, lk);
+  return max((lk + piece - 1) / piece, 1);
 }
 
 template <int DP, bool SPLIT>
@@ -98,120 +181,210 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
   const int32_t kvh = blockIdx.x % a.kv_heads;
   Sequence w;
   if (!find_tile<false>(a, a.tiles - 1 - static_cast<int64_t>(blockIdx.x / a.kv_heads), kRowsLg, w)) return;
-
-  // the lane's row; rows past the last repeat it, and are not stored
-  const int32_t row = w.first + 32 * wave + (lane & 31);
-  const bool valid = row < w.rows;
-  const int32_t i = min(row, w.rows - 1) / a.group;
-  const int64_t head = kvh * a.group + min(row, w.rows - 1) - i * a.group;
-  Rows<DP> x;
-  x.lim = keys_of(a, w, i);
-  x.m = -INFINITY;
-  x.l = 0.0f;
-  const uint16_t* const q = a.q.p + static_cast<int64_t>(w.q0 + i) * a.q.ld_token + head * a.q.ld_head;
-#pragma unroll
-  for (int c = 0; c < H::kChunks; ++c) {
-    const int e = 16 * c + 8 * (lane >> 5);
-    u32x4 u = {0, 0, 0, 0};
-    if (e < a.dim) u = *reinterpret_cast<const u32x4*>(q + e);
-    x.q[c] = __builtin_bit_cast(v8b, u);
+  int32_t part = -1, begin = 0;
+  if (SPLIT) {
+    const int32_t pieces = pieces_of(a, w.lk);
+    if (static_cast<int32_t>(blockIdx.y) >= pieces) return;
+    if (pieces > 1) part = blockIdx.y;
+    begin = static_cast<int32_t>(blockIdx.y) * piece_of(a, w.lk);
   }
-#pragma unroll
-  for (int t = 0; t < H::kTiles; ++t) x.o[t] = zero16();
+  const int32_t row0 = w.first + 32 * wave;
+  const Place at = place_row(a, w, kvh, row0 + (lane & 31));
+  Rows<DP> x;
+  start_rows<DP>(a, w, at, x);
 
   // keys: the wave's first and last row's, the block's last row's
-  const auto token = [&](int32_t row) { return min(row, w.rows - 1) / a.group; };
-  const int32_t least = uniform_i32(keys_of(a, w, token(w.first + 32 * wave)));
-  const int32_t most = uniform_i32(
-      w.first + 32 * wave < w.rows ? keys_of(a, w, token(w.first + 32 * wave + 31)) : 0);
-  int32_t begin = 0, end = uniform_i32(keys_of(a, w, token(w.first + kRows - 1)));
-  if (SPLIT) {
-    const int32_t per = ((w.lk + kKeys - 1) / kKeys + a.splits - 1) / a.splits * kKeys;
-    begin = static_cast<int32_t>(blockIdx.y) * per;
-    end = min(end, begin + per);
-  }
+  const auto keys_at = [&](int32_t row) {
+    return uniform_i32(keys_of(a, w, min(row, w.rows - 1) / a.group));
+  };
+  const int32_t least = keys_at(row0), most = row0 < w.rows ? keys_at(row0 + 31) : 0;
+  int32_t end = keys_at(w.first + kRows - 1);
+  if (SPLIT) end = min(end, begin + piece_of(a, w.lk));
 
   const KeyLoader<DP, kKeys, 4> keys(a, w, kvh, wave);
   const uint32_t base = lds_offset(lds), rows = H::lane_rows(), columns = H::lane_columns();
-  if (begin < end) keys.load(begin, base, wave);
+  if (begin < end) keys.template load<true, true>(begin, base, wave);
   settle(x.q);
   int slot = 0;
   for (int32_t kb = begin; kb < end; kb += kKeys) {
     wait_dma<0>();
-    if (kb + kKeys < end) keys.load(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
-    const uint32_t at = base + slot * 2 * kTile;
-    if (kb < most) tile_step<DP>(x, at + rows, at + kTile + columns, kb, kb + kKeys > least, a.scale * kLog2E);
+    if (kb + kKeys < end) keys.template load<true, true>(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
+    const uint32_t in = base + slot * 2 * kTile;
+    if (kb < most) {
+      Tile<DP, kKeys> tile;
+      tile.scores(x, in + rows);
+      tile.weights(x, kb, kb + kKeys > least, a.scale * kLog2E);
+      tile.values(x, in + kTile + columns);
+    }
     slot ^= 1;
   }
-
   const float sum = x.l + other_half(x.l);
-  const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-  const float lse = sum > 0.0f || sum != sum ? fmaf(x.m, a.scale, kLn2 * __log2f(sum)) : -INFINITY;
-  if (!valid) return;
-  if (SPLIT) {
-    const int64_t at = (static_cast<int64_t>(blockIdx.y) * a.heads + head) * a.tokens_q + w.q0 + i;
-    if (lane < 32) a.part_lse[at] = lse;
-    float* const o = a.part_out + at * a.dim;
+  const float inv = finish_row(a, w, at, part, x.m, sum, lane < 32);
+  if (!at.valid) return;
+#pragma unroll
+  for (int t = 0; t < H::kTiles; ++t) store_out(a, w, at, part, t, x.o[t], inv);
+}
+
+// Few rows (single tokens over a cache): a block takes a piece of a sequence's keys
+// for 32 of its rows at a time, and its two waves every other tile of 32 keys, loaded
+// by the wave for itself: no barrier until the waves' results are joined in LDS.
+// Bound by HBM while enough loads are in flight: k's slot is filled again as soon as
+// the scores are done, v's after its product, so that two tiles of either (32 KB a
+// wave, 128 KB a CU) are on their way at almost any time.
+constexpr int kFewWaves = 4, kFewStep = 32 * kFewWaves;  // keys of all waves' tiles
+template <int DP>
+struct FewRows {
+  typedef Heads<DP> H;
+  static constexpr int kTile = 32 * H::kPitch;
+  static constexpr int kOwn = 2 * kTile;  // of a wave
+  static constexpr int kStats = kFewWaves * kOwn;
+  static constexpr int kBytes = kStats + 2 * kFewWaves * 32 * 4;
+};
+template <int DP>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few_kernel(AttentionArgs a) {
+  typedef Heads<DP> H;
+  typedef FewRows<DP> S;
+  typedef KeyLoader<DP, 32, 1, true> Loader;
+  constexpr int kTile = S::kTile, kN = Loader::kLoads;
+  extern __shared__ __align__(1024) uint8_t lds[];
+  const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6);
+  const int32_t kvh = blockIdx.x % a.kv_heads;
+  const int32_t s = static_cast<int32_t>(blockIdx.x) / a.kv_heads;
+  Sequence w;
+  read_sequence(a, s, w);
+  const int32_t pieces = pieces_of(a, w.lk), piece = piece_of(a, w.lk);
+  if (static_cast<int32_t>(blockIdx.y) >= pieces) return;
+  const int32_t part = pieces > 1 ? static_cast<int32_t>(blockIdx.y) : -1;
+  const int32_t begin = static_cast<int32_t>(blockIdx.y) * piece;
+  const Loader keys(a, w, kvh, 0);
+  const uint32_t base = lds_offset(lds) + wave * S::kOwn;
+  const uint32_t rows = base + H::lane_rows(), columns = base + kTile + H::lane_columns();
+  float* const stats = reinterpret_cast<float*>(lds + S::kStats);
+
+  for (int32_t row0 = 0; row0 < w.rows; row0 += 32) {
+    const Place at = place_row(a, w, kvh, row0 + (lane & 31));
+    Rows<DP> x;
+    start_rows<DP>(a, w, at, x);
+    const int32_t least = uniform_i32(keys_of(a, w, row0 / a.group));
+    const int32_t end = min(begin + piece,
+                            uniform_i32(keys_of(a, w, min(row0 + 31, w.rows - 1) / a.group)));
+    // the wave's tiles: from `first` on, every kFewStep keys
+    const int32_t first = begin + 32 * wave;
+    if (first < end) keys.template load<true, true>(first, base, 0);
+    settle(x.q);
+    for (int32_t kb = first; kb < end; kb += kFewStep) {
+      const bool next = kb + kFewStep < end;
+      Tile<DP, 32> tile;
+      wait_own_dma<kN>();  // (this v is behind this k)
+      tile.scores(x, rows);
+      wait_reads();
+      if (next) keys.template load<true, false>(kb + kFewStep, base, 0);
+      tile.weights(x, kb, kb + 32 > least, a.scale * kLog2E);
+      if (next) wait_own_dma<kN>();
+      else wait_own_dma<0>();
+      tile.values(x, columns);
+      wait_reads();
+      if (next) keys.template load<false, true>(kb + kFewStep, base + kTile, 0);
+    }
+    // the waves' results: the largest maximum, then the sums with their factors
+    const float sum = x.l + other_half(x.l);
+    __syncthreads();
+    if (lane < 32) {
+      stats[wave * 32 + lane] = x.m;
+      stats[(kFewWaves + wave) * 32 + lane] = sum;
+    }
+    float* const sums = reinterpret_cast<float*>(lds);
+    const auto place = [&](int wave, int t, int r) {
+      return sums + ((wave * H::kTiles + t) * 16 + r) * 64 + lane;
+    };
 #pragma unroll
     for (int t = 0; t < H::kTiles; ++t)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d = 32 * t + 8 * g + 4 * (lane >> 5);
-        if (d < a.dim)
-          *reinterpret_cast<u32x4*>(o + d) =
-              u32x4{__float_as_uint(x.o[t][4 * g] * inv), __float_as_uint(x.o[t][4 * g + 1] * inv),
-                    __float_as_uint(x.o[t][4 * g + 2] * inv), __float_as_uint(x.o[t][4 * g + 3] * inv)};
-      }
-  } else {
-    if (a.lse != nullptr && lane < 32) a.lse[head * a.tokens_q + w.q0 + i] = lse;
-    uint16_t* const o = a.out + static_cast<int64_t>(w.q0 + i) * a.ld_out_token + head * a.ld_out_head;
+      for (int r = 0; r < 16; ++r) *place(wave, t, r) = x.o[t][r];
+    __syncthreads();
+    float m = -INFINITY, f[kFewWaves], all = 0.0f;
 #pragma unroll
-    for (int t = 0; t < H::kTiles; ++t)
+    for (int v = 0; v < kFewWaves; ++v) m = fmaxf(m, stats[v * 32 + (lane & 31)]);
+    const float c = a.scale * kLog2E;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d = 32 * t + 8 * g + 4 * (lane >> 5);
-        if (d < a.dim)
-          *reinterpret_cast<u32x2*>(o + d) =
-              u32x2{pack_bf16(x.o[t][4 * g] * inv, x.o[t][4 * g + 1] * inv),
-                    pack_bf16(x.o[t][4 * g + 2] * inv, x.o[t][4 * g + 3] * inv)};
+    for (int v = 0; v < kFewWaves; ++v) {
+      const float n = stats[v * 32 + (lane & 31)], l = stats[(kFewWaves + v) * 32 + (lane & 31)];
+      // (a wave that saw nothing has no part, but a NaN has)
+      f[v] = n == -INFINITY && l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((n - (m == -INFINITY ? 0.0f : m)) * c);
+      all += f[v] * l;
+    }
+    const float inv = finish_row(a, w, at, part, m, all, lane < 32 && wave == 0);
+#pragma unroll 1
+    for (int t = wave; t < H::kTiles; t += kFewWaves) {
+      v16f o;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        o[r] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < kFewWaves; ++v)
+          if (f[v] != 0.0f) o[r] = fmaf(f[v], *place(v, t, r), o[r]);
       }
+      if (at.valid) store_out(a, w, at, part, t, o, inv);
+    }
+    wait_own_dma<0>();  // (the stores: the next rows' loads are counted alone)
+    __syncthreads();
   }
 }
 
-// The splits' results of one token and head joined by a wave: weights
-// exp(lse of the split - lse of all), in the splits' order.
+// The pieces' results of one token and head joined by a block: weights
+// exp(lse of the piece - lse of all) (a piece a lane, at most 64); wave w adds pieces
+// w, w + 4, ... in order, and the waves' sums are added in order.
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t n = static_cast<int64_t>(a.heads) * a.tokens_q;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (at >= n) return;
+  __shared__ float sums[3][128];
+  const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6);
+  const int64_t n = static_cast<int64_t>(a.heads) * a.tokens_q, at = blockIdx.x;
   const int64_t head = at / a.tokens_q, token = at - head * a.tokens_q;
-  if (a.seq_q != nullptr && (token < a.seq_q[0] || token >= a.seq_q[a.sequences])) return;
-  float top = -INFINITY;
-  bool bad = false;
-  for (int32_t s = 0; s < a.splits; ++s) {
-    const float l = a.part_lse[s * n + at];
-    bad |= l != l;
-    top = fmaxf(top, l);
+  int32_t s = 0;
+  if (a.seq_q != nullptr) {
+    s = find_sequence(a.sequences,
+                      [&](int32_t i) { return clamp_token(a.seq_q[i], a.tokens_q) <= token; });
+    if (s < 0) return;
   }
-  float sum = 0.0f, o[2] = {0.0f, 0.0f};
-  const float base = top == -INFINITY ? 0.0f : top;
-  for (int32_t s = 0; s < a.splits; ++s) {
-    const float f = expf(a.part_lse[s * n + at] - base);
-    if (f == 0.0f) continue;
-    sum += f;
-    const float* const p = a.part_out + (s * n + at) * a.dim;
+  Sequence w;
+  read_sequence(a, s, w);
+  if (token >= w.q0 + w.lq) return;
+  const int32_t pieces = pieces_of(a, w.lk);
+  if (pieces == 1) return;  // (written already)
+  const float lse = lane < pieces ? a.part_lse[lane * n + at] : -INFINITY;
+  float top = lse;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (lane + 64 * e < a.dim) o[e] = fmaf(f, p[lane + 64 * e], o[e]);
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float f = expf(lse - (top == -INFINITY ? 0.0f : top));  // (a NaN stays one)
+  float sum = f;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  const int e = 2 * lane;
+  float o[2] = {0.0f, 0.0f};
+#pragma unroll 4
+  for (int32_t p = wave; p < pieces; p += 4) {
+    const float g = __shfl(f, p);
+    float2 v = {0.0f, 0.0f};
+    if (e < a.dim) v = *reinterpret_cast<const float2*>(a.part_out + (p * n + at) * a.dim + e);
+    o[0] = fmaf(g, v.x, o[0]);
+    o[1] = fmaf(g, v.y, o[1]);
   }
-  const float inv = sum > 0.0f || bad ? 1.0f / sum : 0.0f;
-  if (a.lse != nullptr && lane == 0)
-    a.lse[at] = sum > 0.0f || bad ? top + logf(sum) : -INFINITY;
-  uint16_t* const out = a.out + token * a.ld_out_token + head * a.ld_out_head;
+  if (wave > 0) {
+    sums[wave - 1][e] = o[0];
+    sums[wave - 1][e + 1] = o[1];
+  }
+  __syncthreads();
+  if (wave > 0) return;
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
-    if (lane + 64 * e < a.dim) out[lane + 64 * e] = round_bf16(o[e] * inv);
+  for (int v = 0; v < 3; ++v) {
+    o[0] += sums[v][e];
+    o[1] += sums[v][e + 1];
+  }
+  const bool any = sum > 0.0f || sum != sum;
+  const float inv = any ? 1.0f / sum : 0.0f;
+  if (a.lse != nullptr && lane == 0) a.lse[at] = any ? top + logf(sum) : -INFINITY;
+  if (e < a.dim)
+    *reinterpret_cast<uint32_t*>(a.out + token * a.ld_out_token + head * a.ld_out_head + e) =
+        pack_bf16(o[0] * inv, o[1] * inv);
 }
 
 // Tiles of rows (an upper bound, see find_tile).
@@ -219,45 +392,62 @@ int64_t row_tiles(const AttentionArgs& a, int lg) {
   return (a.tokens_q * a.group >> lg) + a.sequences;
 }
 
-// Splits of the keys: where the tiles do not fill the chip, so many that they do,
-// of at least 256 keys each on average.
-int splits_of(const AttentionArgs& a) {
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// How a call is done: few rows a sequence (on average: the lengths are on the
+// device) by sequences and pieces of keys; else by tiles of 128 rows, and pieces of
+// keys where these do not fill the chip.
+struct Form {
+  bool few;
+  int32_t splits, piece;
+};
+Form form_of(const AttentionArgs& a) {
+  const int64_t rows = a.tokens_q * a.group, most = ceil_div(a.tokens_k, 128);
+  if (rows <= 32 * static_cast<int64_t>(a.sequences)) {
+    // pieces of 128 to 1024 keys, so that there are some 512 of them, and so many
+    // of a sequence that one of more than the average length has them too
+    const int64_t blocks = static_cast<int64_t>(a.sequences) * a.kv_heads;
+    const int64_t piece = 128 * std::min<int64_t>(8, std::max<int64_t>(1, a.tokens_k * a.kv_heads / (512 * 128)));
+    const int64_t splits = std::min(ceil_div(a.tokens_k, piece),
+                                    std::max(ceil_div(a.tokens_k, piece * a.sequences), 2048 / blocks));
+    return Form{true, static_cast<int32_t>(std::min<int64_t>(64, std::max<int64_t>(1, splits))),
+                static_cast<int32_t>(piece)};
+  }
   const int64_t blocks = row_tiles(a, kRowsLg) * a.kv_heads;
-  if (blocks >= 384) return 1;
-  const int64_t keys = a.tokens_k / a.sequences;
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(512 / blocks, keys / 256)));
+  const int64_t splits = blocks >= 384 ? 1 : std::min(512 / blocks, std::max<int64_t>(1, most / 2));
+  return Form{false, static_cast<int32_t>(splits), 256};
 }
 
 template <int DP>
-void launch(const AttentionArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<uint32_t>(a.tiles) * a.kv_heads, a.splits);
-  if (a.splits > 1) {
-    hipLaunchKernelGGL((attention_kernel<DP, true>), grid, dim3(256), 0, s, a);
-    const int64_t n = static_cast<int64_t>(a.heads) * a.tokens_q;
-    hipLaunchKernelGGL(attention_join_kernel, dim3(static_cast<uint32_t>((n + 3) / 4)), dim3(256), 0,
-                       s, a);
-  } else {
-    hipLaunchKernelGGL((attention_kernel<DP, false>), grid, dim3(256), 0, s, a);
-  }
+void launch(const AttentionArgs& a, bool few, hipStream_t s) {
+  const dim3 grid(static_cast<uint32_t>(few ? a.sequences : a.tiles) * a.kv_heads, a.splits);
+  constexpr int kFewBytes = FewRows<DP>::kBytes;
+  if (few) hipLaunchKernelGGL((attention_few_kernel<DP>), grid, dim3(64 * kFewWaves), kFewBytes, s, a);
+  else if (a.splits > 1) hipLaunchKernelGGL((attention_kernel<DP, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attention_kernel<DP, false>), grid, dim3(256), 0, s, a);
+  if (a.splits == 1) return;
+  const int64_t n = static_cast<int64_t>(a.heads) * a.tokens_q;
+  hipLaunchKernelGGL(attention_join_kernel, dim3(static_cast<uint32_t>(n)), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
 size_t attention_workspace(const AttentionArgs& a) {
-  const int n = splits_of(a);
-  if (n == 1) return 0;
-  return static_cast<size_t>(n) * a.heads * a.tokens_q * (a.dim + 1) * sizeof(float);
+  const int64_t n = form_of(a).splits;
+  return n == 1 ? 0 : static_cast<size_t>(n * a.heads * a.tokens_q * (a.dim + 1)) * sizeof(float);
 }
 
 hipError_t launch_attention(AttentionArgs a, void* ws, hipStream_t s) {
   (void)hipGetLastError();
   a.tiles = static_cast<int32_t>(row_tiles(a, kRowsLg));
-  a.splits = splits_of(a);
+  const Form form = form_of(a);
+  a.splits = form.splits;
+  a.piece = form.piece;
   a.part_out = static_cast<float*>(ws);
   a.part_lse = a.part_out + static_cast<int64_t>(a.splits) * a.heads * a.tokens_q * a.dim;
-  if (a.dim <= 64) launch<64>(a, s);
-  else if (a.dim <= 96) launch<96>(a, s);
-  else launch<128>(a, s);
+  if (a.dim <= 64) launch<64>(a, form.few, s);
+  else if (a.dim <= 96) launch<96>(a, form.few, s);
+  else launch<128>(a, form.few, s);
   return hipGetLastError();
 }
 

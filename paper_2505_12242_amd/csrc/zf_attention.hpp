@@ -116,7 +116,8 @@ struct AttentionArgs {
   int64_t tokens_q, tokens_k;
   int32_t sequences, heads, kv_heads, group, dim, causal;
   int32_t tiles;   // of rows, of one key head (an upper bound)
-  int32_t splits;  // of the keys
+  int32_t splits;  // of the keys, the most; piece: keys of one, the least (128 n)
+  int32_t piece;
   float scale;
   float* part_out;  // [splits][heads][tokens_q][dim]
   float* part_lse;  // [splits][heads][tokens_q]
@@ -132,35 +133,27 @@ __device__ __forceinline__ int32_t clamp_token(int32_t x, int64_t tokens) {
   return x < 0 ? 0 : x > tokens ? static_cast<int32_t>(tokens) : x;
 }
 
-// Tile `g` of the tiles of 2^lg rows (KEYS: of keys): sequence s has the tiles
-// from (start * group >> lg) + s on, which are at least as many as it needs
-// before the next one's.  So no list of tiles is built, and a captured call
-// follows the lengths.  The wave searches 64 sequences at a time.  False: no
-// such tile.
-template <bool KEYS, typename Args>
-__device__ __forceinline__ bool find_tile(const Args& a, int64_t g, int lg, Sequence& w) {
-  const int64_t group = KEYS ? 1 : a.group;
+// The last of `count` sequences for which before(i) holds (it does up to some i),
+// or -1.  The wave searches 64 at a time.
+template <typename F>
+__device__ __forceinline__ int32_t find_sequence(int32_t count, const F& before) {
+  const int lane = threadIdx.x & 63;
   int32_t s = 0;
+  do {
+    const int32_t step = (count + 63) / 64;
+    const int64_t at = static_cast<int64_t>(lane) * step;
+    const uint64_t found = __ballot(at < count && before(s + static_cast<int32_t>(at)));
+    if (found == 0) return -1;
+    const int32_t last = 63 - __builtin_clzll(found);
+    s += last * step;
+    count = min(step, count - last * step);
+  } while (count > 1);
+  return uniform_i32(s);
+}
+
+template <typename Args>
+__device__ __forceinline__ void read_sequence(const Args& a, int32_t s, Sequence& w) {
   if (a.seq_q != nullptr) {
-    const int32_t* const starts = KEYS ? a.seq_k : a.seq_q;
-    const int64_t tokens = KEYS ? a.tokens_k : a.tokens_q;
-    const int lane = threadIdx.x & 63;
-    int32_t count = a.sequences;
-    do {
-      const int32_t step = (count + 63) / 64;
-      const int64_t at = static_cast<int64_t>(lane) * step;
-      bool ok = false;
-      if (at < count) {
-        const int32_t i = s + static_cast<int32_t>(at);
-        ok = (clamp_token(starts[i], tokens) * group >> lg) + i <= g;
-      }
-      const uint64_t found = __ballot(ok);
-      if (found == 0) return false;
-      const int32_t last = 63 - __builtin_clzll(found);
-      s += last * step;
-      count = min(step, count - last * step);
-    } while (count > 1);
-    s = uniform_i32(s);
     w.q0 = clamp_token(a.seq_q[s], a.tokens_q);
     w.lq = max(clamp_token(a.seq_q[s + 1], a.tokens_q) - w.q0, 0);
     w.k0 = clamp_token(a.seq_k[s], a.tokens_k);
@@ -176,6 +169,25 @@ __device__ __forceinline__ bool find_tile(const Args& a, int64_t g, int lg, Sequ
   w.k0 = uniform_i32(w.k0);
   w.lk = uniform_i32(w.lk);
   w.rows = w.lq * a.group;
+}
+
+// Tile `g` of the tiles of 2^lg rows (KEYS: of keys): sequence s has the tiles
+// from (start * group >> lg) + s on, which are at least as many as it needs
+// before the next one's.  So no list of tiles is built, and a captured call
+// follows the lengths.  False: no such tile.
+template <bool KEYS, typename Args>
+__device__ __forceinline__ bool find_tile(const Args& a, int64_t g, int lg, Sequence& w) {
+  const int64_t group = KEYS ? 1 : a.group;
+  int32_t s = 0;
+  if (a.seq_q != nullptr) {
+    const int32_t* const starts = KEYS ? a.seq_k : a.seq_q;
+    const int64_t tokens = KEYS ? a.tokens_k : a.tokens_q;
+    s = find_sequence(a.sequences, [&](int32_t i) {
+      return (clamp_token(starts[i], tokens) * group >> lg) + i <= g;
+    });
+    if (s < 0) return false;
+  }
+  read_sequence(a, s, w);
   const int64_t first = (g - (((KEYS ? w.k0 : w.q0) * group >> lg) + s)) << lg;
   if (first >= (KEYS ? w.lk : w.rows)) return false;
   w.first = static_cast<int32_t>(first);
@@ -196,12 +208,19 @@ __device__ __forceinline__ uint32_t lds_offset(const uint8_t* lds) {
   return static_cast<uint32_t>(uniform_i32(static_cast<int32_t>(reinterpret_cast<uintptr_t>(
       (const __attribute__((address_space(3))) uint8_t*)lds))));
 }
+template <bool NT = false>
 __device__ __forceinline__ void dma16(rsrc_t r, uint32_t lds, uint32_t voff) {
 #ifdef __HIP_DEVICE_COMPILE__
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
-                   lds),
-               "v"(voff), "s"(r)
-               : "memory", "m0");
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(
+                     lds),
+                 "v"(voff), "s"(r)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
+                     lds),
+                 "v"(voff), "s"(r)
+                 : "memory", "m0");
 #endif
 }
 __device__ __forceinline__ void dma4(rsrc_t r, uint32_t lds, uint32_t voff) {
@@ -234,10 +253,14 @@ __device__ __forceinline__ void wait_own_dma() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// Waits until the wave's reads of LDS are done: what they read may be overwritten.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Loads tiles of N keys of k and v: the wave's part of each (`waves` of them load
 // together), rows past the last key repeating it, units past the head's width
-// the last one (the other operand is zero there, or the result not stored).
-template <int DP, int N, int WAVES>
+// the last one (the other operand is zero there, or the result not stored).  NT:
+// each is read by one block (nontemporal).
+template <int DP, int N, int WAVES, bool NT = false>
 struct KeyLoader {
   typedef Heads<DP> H;
   static constexpr int kLoads = N / H::kPer / WAVES;  // of a wave, of either
@@ -266,22 +289,27 @@ struct KeyLoader {
   static __device__ __forceinline__ uint32_t offset(int32_t row, int64_t ld) {
     return static_cast<uint32_t>(row) * (static_cast<uint32_t>(ld) * 2);
   }
-  // Keys kb .. kb + N - 1 to byte `lds`, k's first, v's kTile behind them.  kb < keys.
+  // Keys kb .. kb + N - 1 of k, of v, or of both (v's kTile behind k's), to byte
+  // `lds`.  kb < keys.
+  template <bool K, bool V>
   __device__ __forceinline__ void load(int32_t kb, uint32_t lds, int wave) const {
     const rsrc_t rk = make_rsrc(k + kb * ldk, -1), rv = make_rsrc(v + kb * ldv, -1);
     lds += wave * kLoads * 1024;
+    const uint32_t to_v = K ? lds + kTile : lds;
     if (kb + N <= keys) {
 #pragma unroll
-      for (int n = 0; n < kLoads; ++n) dma16(rk, lds + n * 1024, at[0][n]);
+      for (int n = 0; n < kLoads; ++n)
+        if (K) dma16<NT>(rk, lds + n * 1024, at[0][n]);
 #pragma unroll
-      for (int n = 0; n < kLoads; ++n) dma16(rv, lds + kTile + n * 1024, at[1][n]);
+      for (int n = 0; n < kLoads; ++n)
+        if (V) dma16<NT>(rv, to_v + n * 1024, at[1][n]);
     } else {
 #pragma unroll
       for (int n = 0; n < kLoads; ++n)
-        dma16(rk, lds + n * 1024, offset(min(row[n], keys - 1 - kb), ldk) + unit[n]);
+        if (K) dma16<NT>(rk, lds + n * 1024, offset(min(row[n], keys - 1 - kb), ldk) + unit[n]);
 #pragma unroll
       for (int n = 0; n < kLoads; ++n)
-        dma16(rv, lds + kTile + n * 1024, offset(min(row[n], keys - 1 - kb), ldv) + unit[n]);
+        if (V) dma16<NT>(rv, to_v + n * 1024, offset(min(row[n], keys - 1 - kb), ldv) + unit[n]);
     }
   }
 };

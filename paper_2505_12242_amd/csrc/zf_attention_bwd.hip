@@ -115,13 +115,13 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
   const int32_t end = uniform_i32(keys_of(a, w, token_of(w.first + kBlock - 1)));
   const KeyLoader<DP, kKeys, 4> keys(a, w, kvh, wave);
   const uint32_t base = lds_offset(lds), rows = H::lane_rows(), columns = H::lane_columns();
-  if (end > 0) keys.load(0, base, wave);
+  if (end > 0) keys.template load<true, true>(0, base, wave);
   settle(q);
   settle(dout);
   int slot = 0;
   for (int32_t kb = 0; kb < end; kb += kKeys) {
     wait_dma<0>();
-    if (kb + kKeys < end) keys.load(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
+    if (kb + kKeys < end) keys.template load<true, true>(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
     const uint32_t at = base + slot * 2 * kTile;
     const uint32_t k = at + rows, kt = at + columns, v = at + kTile + rows;
     if (kb < most) {

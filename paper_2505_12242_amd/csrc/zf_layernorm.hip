@@ -3,10 +3,10 @@
 //
 // Rows and blocks as for the RMS norm (zf_norm.hip): one block per row, the row
 // in registers, every input read once and every output written once, sums in
-// fp32.  The mean and the sum of squares about it take one barrier: each wave
-// has its own mean and its squares about that one (both over the wave alone),
-// and the waves' are joined as m2 + n (mean of the wave - mean)^2.  Nothing
-// cancels, as a sum of squares less a squared sum would.
+// fp32.  The squares are summed about the mean, in a second pass over the
+// registers and a second barrier: nothing cancels, as a sum of squares less a
+// squared sum would.  (Each wave's squares about its own mean, joined with one
+// barrier, cost more than the barrier: 8192 x 5120 bf16 144 us.)
 #include <algorithm>
 
 #include "zf_norm.hpp"
@@ -41,58 +41,40 @@ struct Moments {
 
 // The row's moments in every thread: piece i of V of the thread's 8 elements
 // are columns (threadIdx.x + i * NT) * 8 and on, zeros past the row's end.
-// `red` as block_sum's.
+// `red`: two of block_sum's.
 template <typename T, int NT, int V>
 __device__ __forceinline__ Moments moments(const Vec8<T> (&h)[V], int64_t cols, float eps,
                                            float (&red)[2][NT / 64]) {
-  const int wave = threadIdx.x >> 6;
+  const float inv = 1.0f / static_cast<float>(cols > 0 ? cols : 1);
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) s += h[i][j];
-  s = wave_sum(s);
-  const auto count = [&](int w) {  // of wave w's elements
-    int64_t n = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      n += max(int64_t(0), min(int64_t(512), cols - (w * 64 + i * NT) * 8));
-    return static_cast<float>(n);
-  };
-  const float own = count(wave), mu = own > 0.0f ? s / own : 0.0f;
+  const float mean = block_sum<NT>(s, red[0]) * inv;
   float m2 = 0.0f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int64_t valid = cols - (threadIdx.x + i * NT) * 8;
+    if (valid >= 8) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float d = j < valid ? h[i][j] - mu : 0.0f;
-      m2 += d * d;
+      for (int j = 0; j < 8; ++j) {
+        const float d = h[i][j] - mean;
+        m2 += d * d;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float d = j < valid ? h[i][j] - mean : 0.0f;
+        m2 += d * d;
+      }
     }
   }
-  m2 = wave_sum(m2);
-  const float n = static_cast<float>(cols > 0 ? cols : 1);
-  if constexpr (NT == 64) return Moments{s / n, 1.0f / sqrtf(m2 / n + eps)};
-  if ((threadIdx.x & 63) == 0) {
-    red[0][wave] = s;
-    red[1][wave] = m2;
-  }
-  __syncthreads();
-  float sum = 0.0f;
-#pragma unroll
-  for (int w = 0; w < NT / 64; ++w) sum += red[0][w];
-  const float mean = sum / n;
-  float all = 0.0f;
-#pragma unroll
-  for (int w = 0; w < NT / 64; ++w) {
-    const float k = count(w), d = k > 0.0f ? red[0][w] / k - mean : 0.0f;
-    all += red[1][w] + k * (d * d);
-  }
-  return Moments{mean, 1.0f / sqrtf(all / n + eps)};
+  return Moments{mean, 1.0f / sqrtf(block_sum<NT>(m2, red[1]) * inv + eps)};
 }
 
 template <typename T, int NT, int V, bool RES>
-__global__ __launch_bounds__(NT) void layernorm_kernel(LayerNormArgs a) {
+__global__ __launch_bounds__(NT, V == 1 ? 8 : 1) void layernorm_kernel(LayerNormArgs a) {
   __shared__ float red[2][2][NT / 64];
   int flip = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
