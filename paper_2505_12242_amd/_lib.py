@@ -312,8 +312,20 @@ def _workspace(t: Optional[torch.Tensor]) -> int:
     return t.numel() * t.element_size()
 
 
+_gpus = None
+
+
+def _many_gpus() -> bool:
+    """Whether there is more than one GPU that tensors could live on."""
+    global _gpus
+    if _gpus is None:
+        _gpus = torch.cuda.device_count()
+    return _gpus > 1
+
+
 def _same_device(stream, **tensors) -> None:
-    """Refuses tensors of different GPUs, and of another one than the launch's."""
+    """Refuses tensors of different GPUs, and of another one than the launch's.
+    (Called where _many_gpus() says so.)"""
     first = None
     for name, t in tensors.items():
         if t is None or not t.is_cuda:

@@ -28,68 +28,118 @@ struct Rows {
   int32_t lim;   // keys that the lane's row sees
 };
 
-// One tile of KEYS keys, from key kb of the sequence on, its scores and its
-// values.  mask: some row sees only some of them.
-template <int DP, int KEYS>
-struct Tile {
-  typedef Heads<DP> H;
-  v16f s[KEYS / 32];
-  v8b p[KEYS / 16];
+// A weight of 0 hides no infinity and no NaN from a product.  So where some row does
+// not see keys that others do, such elements of v become zeros in LDS, before the
+// product, and are added behind the loop, to the rows that see them (add_odd).
 
-  __device__ __forceinline__ void scores(const Rows<DP>& w, uint32_t k) {
+// The halves of a word whose exponent is all ones, as 0x8000 each.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t x) {
+  return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+// Clears them in N KB of LDS from byte `at` on.  Whether there were any.
+template <int N>
+__device__ __forceinline__ bool scrub(uint32_t at) {
+  uint32_t any = 0;
 #pragma unroll
-    for (int t = 0; t < KEYS / 32; ++t) {
-      s[t] = zero16();
+  for (int n = 0; n < N; ++n) {
+    auto* const p = (__attribute__((address_space(3))) u32x4*)(at + n * 1024 + 16 * (threadIdx.x & 63));
+    u32x4 x = *p;
+    uint32_t odd = 0;
 #pragma unroll
-      for (int j = 0; j < H::kChunks; ++j) s[t] = mma(H::frag(k, 32 * t, j), w.q[j], s[t]);
+    for (int i = 0; i < 4; ++i) odd |= odd_halves(x[i]);
+    if (odd != 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] &= ~((odd_halves(x[i]) >> 15) * 0xffffu);
+      *p = x;
     }
-    __builtin_amdgcn_sched_barrier(0);
+    any |= odd;
   }
-  __device__ __forceinline__ void weights(Rows<DP>& w, int32_t kb, bool mask, float c) {
-    if (mask) {
-      const int half = threadIdx.x >> 5 & 1;
-#pragma unroll
-      for (int t = 0; t < KEYS / 32; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (kb + 32 * t + reg_row(r) + 4 * half >= w.lim) s[t][r] = -INFINITY;
+  return any != 0;
+}
+// Adds what scrub cleared of keys [from, to).
+template <int DP>
+__device__ __noinline__ void add_odd(const uint16_t* v, int64_t ld, int32_t dim, int32_t from,
+                                     int32_t to, int32_t lim, float* o) {
+  for (int32_t key = from; key < min(to, lim); ++key)
+    for (int d = 4 * (threadIdx.x >> 5 & 1); d < dim; d += 8) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(v + key * ld + d);
+      if ((odd_halves(x.x) | odd_halves(x.y)) == 0) continue;
+      for (int e = 0; e < 4; ++e) {
+        const float f = widen_bf16(static_cast<uint16_t>((e & 2 ? x.y : x.x) >> (16 * (e & 1))));
+        if (!(fabsf(f) < INFINITY)) o[d / 8 * 4 + e] += f;
+      }
     }
-    float top = -INFINITY;
+}
+template <int DP>
+__device__ __forceinline__ void add_odd(const AttentionArgs& a, const Sequence& w, int32_t kvh,
+                                        int32_t from, int32_t to, Rows<DP>& x) {
+  float o[DP / 2];
+#pragma unroll
+  for (int i = 0; i < DP / 2; ++i) o[i] = x.o[i / 16][i % 16];
+  add_odd<DP>(a.v.p + kvh * a.v.ld_head + w.k0 * a.v.ld_token, a.v.ld_token, a.dim, from, to, x.lim, o);
+#pragma unroll
+  for (int i = 0; i < DP / 2; ++i) x.o[i / 16][i % 16] = o[i];
+}
+
+// One tile of KEYS keys, from key kb of the sequence on.  MASK: some row may see only
+// some of them.  k is read before after_scores, v behind before_values.
+template <int DP, int KEYS, bool MASK, typename F, typename G>
+__device__ __forceinline__ void tile_step(Rows<DP>& w, uint32_t k, uint32_t v, int32_t kb, float c,
+                                          const F& after_scores,
+                                          const G& before_values) {
+  typedef Heads<DP> H;
+  const int half = threadIdx.x >> 5 & 1;
+  v16f s[KEYS / 32];
+#pragma unroll
+  for (int t = 0; t < KEYS / 32; ++t) {
+    s[t] = zero16();
+#pragma unroll
+    for (int j = 0; j < H::kChunks; ++j) s[t] = mma(H::frag(k, 32 * t, j), w.q[j], s[t]);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  after_scores();
+  if (MASK) {
 #pragma unroll
     for (int t = 0; t < KEYS / 32; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-    top = fmaxf(top, other_half(top));
-    // (the first tile that a row sees anything of has m = -infinity)
-    if (__any(top * c > w.m * c + 8.0f)) {
-      const float m = fmaxf(w.m, top);
-      const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((w.m - m) * c);
-      w.m = m;
-      w.l *= f;
-#pragma unroll
-      for (int t = 0; t < H::kTiles; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) w.o[t][r] *= f;
-    }
-    const float mc = w.m == -INFINITY ? 0.0f : w.m * c;
-#pragma unroll
-    for (int t = 0; t < KEYS / 32; ++t) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c, -mc));
-        w.l += s[t][r];
-      }
-      p[2 * t] = pack8(s[t], 0);
-      p[2 * t + 1] = pack8(s[t], 1);
-    }
+      for (int r = 0; r < 16; ++r)
+        if (kb + 32 * t + reg_row(r) + 4 * half >= w.lim) s[t][r] = -INFINITY;
   }
-  __device__ __forceinline__ void values(Rows<DP>& w, uint32_t v) const {
+  float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < KEYS / 16; ++j)
+  for (int t = 0; t < KEYS / 32; ++t)
 #pragma unroll
-      for (int t = 0; t < H::kTiles; ++t) w.o[t] = mma(H::frag_t(v, 16 * j, t), p[j], w.o[t]);
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+  top = fmaxf(top, other_half(top));
+  // (the first tile that a row sees anything of has m = -infinity)
+  if (__any(top * c > w.m * c + 8.0f)) {
+    const float m = fmaxf(w.m, top);
+    const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((w.m - m) * c);
+    w.m = m;
+    w.l *= f;
+#pragma unroll
+    for (int t = 0; t < H::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w.o[t][r] *= f;
   }
-};
+  const float mc = w.m == -INFINITY ? 0.0f : w.m * c;
+  v8b p[KEYS / 16];
+#pragma unroll
+  for (int t = 0; t < KEYS / 32; ++t) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c, -mc));
+      w.l += s[t][r];
+    }
+    p[2 * t] = pack8(s[t], 0);
+    p[2 * t + 1] = pack8(s[t], 1);
+  }
+  before_values();
+#pragma unroll
+  for (int j = 0; j < KEYS / 16; ++j)
+#pragma unroll
+    for (int t = 0; t < H::kTiles; ++t) w.o[t] = mma(H::frag_t(v, 16 * j, t), p[j], w.o[t]);
+}
 
 // The lane's row: row `row` of the sequence, or its last where there are fewer
 // (`valid`: it is the row itself).
@@ -197,7 +247,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
   const auto keys_at = [&](int32_t row) {
     return uniform_i32(keys_of(a, w, min(row, w.rows - 1) / a.group));
   };
-  const int32_t least = keys_at(row0), most = row0 < w.rows ? keys_at(row0 + 31) : 0;
+  const int32_t most = row0 < w.rows ? keys_at(row0 + 31) : 0;
   int32_t end = keys_at(w.first + kRows - 1);
   if (SPLIT) end = min(end, begin + piece_of(a, w.lk));
 
@@ -205,19 +255,26 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
   const uint32_t base = lds_offset(lds), rows = H::lane_rows(), columns = H::lane_columns();
   if (begin < end) keys.template load<true, true>(begin, base, wave);
   settle(x.q);
-  int slot = 0;
-  for (int32_t kb = begin; kb < end; kb += kKeys) {
+  // the tiles that every row sees whole, then the others
+  const int32_t whole = keys_at(w.first);
+  int slot = 0, odd = 0;
+  int32_t kb = begin;
+  const auto step = [&](auto mask) {
     wait_dma<0>();
-    if (kb + kKeys < end) keys.template load<true, true>(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
+    if (kb + kKeys < end)
+      keys.template load<true, true>(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
     const uint32_t in = base + slot * 2 * kTile;
-    if (kb < most) {
-      Tile<DP, kKeys> tile;
-      tile.scores(x, in + rows);
-      tile.weights(x, kb, kb + kKeys > least, a.scale * kLog2E);
-      tile.values(x, in + kTile + columns);
-    }
+    if (mask.value && whole < w.lk)
+      odd |= __syncthreads_or(scrub<kTile / 4096>(in + kTile + wave * (kTile / 4)));
+    if (kb < most)
+      tile_step<DP, kKeys, mask.value>(x, in + rows, in + kTile + columns, kb, a.scale * kLog2E,
+                                       [] {}, [] {});
+    pin(x.o);
     slot ^= 1;
-  }
+  };
+  for (; kb < end && kb + kKeys <= whole; kb += kKeys) step(std::false_type());
+  for (; kb < end; kb += kKeys) step(std::true_type());
+  if (odd) add_odd<DP>(a, w, kvh, max(begin, whole / kKeys * kKeys), end, x);
   const float sum = x.l + other_half(x.l);
   const float inv = finish_row(a, w, at, part, x.m, sum, lane < 32);
   if (!at.valid) return;
@@ -272,20 +329,31 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few_kernel(Attent
     const int32_t first = begin + 32 * wave;
     if (first < end) keys.template load<true, true>(first, base, 0);
     settle(x.q);
-    for (int32_t kb = first; kb < end; kb += kFewStep) {
+    int32_t kb = first;
+    bool odd = false;
+    const auto step = [&](auto mask) {
       const bool next = kb + kFewStep < end;
-      Tile<DP, 32> tile;
       wait_own_dma<kN>();  // (this v is behind this k)
-      tile.scores(x, rows);
-      wait_reads();
-      if (next) keys.template load<true, false>(kb + kFewStep, base, 0);
-      tile.weights(x, kb, kb + 32 > least, a.scale * kLog2E);
-      if (next) wait_own_dma<kN>();
-      else wait_own_dma<0>();
-      tile.values(x, columns);
+      tile_step<DP, 32, mask.value>(
+          x, rows, columns, kb, a.scale * kLog2E,
+          [&] {
+            wait_reads();
+            if (next) keys.template load<true, false>(kb + kFewStep, base, 0);
+          },
+          [&] {
+            if (next) wait_own_dma<kN>();
+            else wait_own_dma<0>();
+            if (mask.value && least < w.lk) odd |= scrub<S::kTile / 1024>(base + kTile);
+          });
       wait_reads();
       if (next) keys.template load<false, true>(kb + kFewStep, base + kTile, 0);
-    }
+      pin(x.o);
+    };
+    for (; kb < end && kb + 32 <= least; kb += kFewStep) step(std::false_type());
+    const int32_t from = kb;
+    for (; kb < end; kb += kFewStep) step(std::true_type());
+    if (__any(odd))
+      for (int32_t t = from; t < end; t += kFewStep) add_odd<DP>(a, w, kvh, t, min(t + 32, end), x);
     // the waves' results: the largest maximum, then the sums with their factors
     const float sum = x.l + other_half(x.l);
     __syncthreads();

@@ -769,7 +769,8 @@ void launch_linear(const MatmulArgs& a, const Epilogue& e, void* ws, hipStream_t
       launch_rows<Linear<T, ACT>>(a, e, s);
       return;
     }
-    // (a scale group spans 8 blocks of 16 columns)
+    // (A scale group spans 8 blocks of 16 columns.  Blocks of a whole group would need
+    // no second launch, but leave most CUs idle: 8 x 11008 x 4096 31 us, not 18.6.)
     MatmulArgs b = a;
     b.out = ws;
     b.ld_out = a.n;

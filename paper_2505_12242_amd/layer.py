@@ -19,8 +19,8 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
-from ._lib import (LIB, AdamHparams, ZfAdamwTensor, ZfEpilogue, ZfFp8, _check, _empty, _mat, _ptr,
-                   _same_device, _stream, _vec, _workspace, c_sz, c_vp)
+from ._lib import (LIB, AdamHparams, ZfAdamwTensor, ZfEpilogue, ZfFp8, _check, _empty, _many_gpus, _mat,
+                   _ptr, _same_device, _stream, _vec, _workspace, c_sz, c_vp)
 
 DTYPES = {torch.bfloat16: 0, torch.float32: 1}  # zf_dtype
 DATA, SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
@@ -301,8 +301,9 @@ def layernorm(x: torch.Tensor, gain: torch.Tensor, bias: Optional[torch.Tensor] 
     if bias is not None:
         _vec(bias, gain.dtype, "bias", c)
     dtype, dev = x.dtype, x.device
-    _same_device(stream, x=x, gain=gain, bias=bias, residual=residual, h=h, y=y, mean=mean,
-                 rstd=rstd, **_fp8_parts(q=q))
+    if _many_gpus():
+        _same_device(stream, x=x, gain=gain, bias=bias, residual=residual, h=h, y=y, mean=mean,
+                     rstd=rstd, **_fp8_parts(q=q))
     if mean is None:
         mean = _empty(r, torch.float32, dev, stream)
     else:
@@ -356,8 +357,9 @@ def layernorm_backward(dy: torch.Tensor, h: torch.Tensor, gain: torch.Tensor, me
     _vec(gain, gain.dtype, "gain", c)
     _vec(mean, torch.float32, "mean", r)
     _vec(rstd, torch.float32, "rstd", r)
-    _same_device(stream, dy=dy, h=h, gain=gain, mean=mean, rstd=rstd, dresidual=dresidual, dx=dx,
-                 dgain=dgain, dbias=dbias, workspace=workspace)
+    if _many_gpus():
+        _same_device(stream, dy=dy, h=h, gain=gain, mean=mean, rstd=rstd, dresidual=dresidual, dx=dx,
+                     dgain=dgain, dbias=dbias, workspace=workspace)
     ld_res = 0
     if dresidual is not None:
         ld_res = _mat(dresidual, dy.dtype, "dresidual", r, c)
@@ -422,8 +424,9 @@ def linear_fp8(a: Fp8, b: Fp8, bias: Optional[torch.Tensor] = None,
     n = b.data.shape[0]
     c_a, c_b = a.as_c("a"), b.as_c("b", None, k)
     dev = a.data.device
-    _same_device(stream, **_fp8_parts(a=a, b=b, q=q), bias=bias, residual=residual, y=y, z=z,
-                 workspace=workspace)
+    if _many_gpus():
+        _same_device(stream, **_fp8_parts(a=a, b=b, q=q), bias=bias, residual=residual, y=y, z=z,
+                     workspace=workspace)
     for t in (residual, y, z):
         if t is not None:
             dtype = t.dtype
@@ -503,8 +506,9 @@ def linear_fp8_backward(dy: torch.Tensor, z: Optional[torch.Tensor] = None,
         ld_z = _mat(z, dy.dtype, "z", r, c)
     else:
         z = None
-    _same_device(stream, dy=dy, z=z, dz=dz, dbias=dbias, workspace=workspace,
-                 **_fp8_parts(q=q, qt=qt))
+    if _many_gpus():
+        _same_device(stream, dy=dy, z=z, dz=dz, dbias=dbias, workspace=workspace,
+                     **_fp8_parts(q=q, qt=qt))
     ld_dz, c_q, c_qt = c, None, None
     if dz is not None:
         ld_dz = _mat(dz, dy.dtype, "dz", r, c)

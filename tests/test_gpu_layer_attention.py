@@ -128,6 +128,10 @@ CASES = [
     dict(lens=[(90, 150)], heads=2, dim=128, std=6.0),       # scores of some hundreds
     dict(lens=[(200, 200)], heads=2, dim=64, scale=1e-3),
     dict(lens=[(31, 2000)], heads=4, kv=2, dim=128),
+    # gradients by blocks of 128 keys, one group of waves or two
+    dict(lens=[(150, 200), (260, 260), (33, 190)] * 3, heads=32, kv=32, dim=72),
+    dict(lens=[(150, 200), (260, 260), (33, 190)] * 3, heads=32, kv=32, dim=128, causal=False),
+    dict(lens=[(150, 200), (260, 260), (70, 190)] * 3, heads=40, kv=20, dim=64),
 ]
 
 
@@ -245,6 +249,40 @@ def test_differences():
             # out enters with its rounding to bf16 (D), p and dS with theirs, the
             # gradient with its own: four roundings of what is summed, at most
             assert abs(slope - (g * d).sum()) <= 4 * H * (g * d).abs().sum() * 3
+
+
+@pytest.mark.parametrize("lens,heads,kv,dim", [([(70, 70), (40, 40)], 2, 2, 64),
+                                               ([(200, 260)], 4, 1, 128), ([(5, 9)], 8, 2, 80),
+                                               ([(4, 300), (1, 7)], 4, 2, 96)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_hidden_keys_reach_nothing(lens, heads, kv, dim, value, which):
+    """A key that is not finite changes the queries that see it, and no other."""
+    c = Case(lens, heads, kv, dim)
+    want = c.run()
+    for at in {lens[0][1] - 1, lens[0][1] // 2}:
+        d = Case(lens, heads, kv, dim)
+        (d.gk if which == "k" else d.gv)[d.ks[0] + at, 0, 3] = value
+        got = d.run()
+        lq, lk = lens[0]
+        mask = seen(lq, lk, True)[:, at].cuda()
+        group = heads // kv
+        for h in range(heads):
+            a, b = got.out[d.qs[0]:d.qs[1], h], want.out[d.qs[0]:d.qs[1], h]
+            if h >= group:  # another key head's
+                assert torch.equal(a, b)
+                continue
+            assert torch.equal(a[~mask], b[~mask])
+            if which == "k":
+                # a score of minus infinity hides the key, others are NaN in the end
+                bad = ~torch.isfinite(a[mask]).all(1)
+                s = c.q[d.qs[0]:d.qs[1], h, 3].cuda()[mask].float() * value
+                assert (bad == (s != -math.inf)).all()
+            else:
+                assert torch.equal(a[mask][:, :3], b[mask][:, :3])
+                x = a[mask][:, 3].float()
+                assert x.isnan().all() if value != value else (x == value).all()
+        assert torch.equal(got.out[d.qs[1]:d.qs[-1]], want.out[d.qs[1]:d.qs[-1]])
 
 
 def test_captured_call_follows_the_lengths():
