@@ -399,13 +399,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few_kernel(Attent
   }
 }
 
-// The pieces' results of one token and head joined by a block: weights
-// exp(lse of the piece - lse of all) (a piece a lane, at most 64); wave w adds pieces
-// w, w + 4, ... in order, and the waves' sums are added in order.
+// The pieces' results of one token and head joined by W waves: weights exp(lse of the
+// piece - lse of all) (a piece a lane, at most 64); wave w adds pieces w, w + W, ...
+// in order, and the waves' sums are added in order.  W 4 where there are many pieces,
+// 1 where many rows (512 tokens x 32 heads in 4 pieces: @@ us, with 4 waves @@).
+template <int W>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
-  __shared__ float sums[3][128];
-  const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6);
-  const int64_t n = static_cast<int64_t>(a.heads) * a.tokens_q, at = blockIdx.x;
+  __shared__ float sums[W > 1 ? W - 1 : 1][128];
+  const int lane = threadIdx.x & 63, index = uniform_i32(threadIdx.x >> 6);
+  const int wave = W == 1 ? 0 : index;
+  const int64_t n = static_cast<int64_t>(a.heads) * a.tokens_q;
+  const int64_t at = W == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + index : blockIdx.x;
+  if (at >= n) return;
   const int64_t head = at / a.tokens_q, token = at - head * a.tokens_q;
   int32_t s = 0;
   if (a.seq_q != nullptr) {
@@ -429,23 +434,25 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
   const int e = 2 * lane;
   float o[2] = {0.0f, 0.0f};
 #pragma unroll 4
-  for (int32_t p = wave; p < pieces; p += 4) {
+  for (int32_t p = wave; p < pieces; p += W) {
     const float g = __shfl(f, p);
     float2 v = {0.0f, 0.0f};
     if (e < a.dim) v = *reinterpret_cast<const float2*>(a.part_out + (p * n + at) * a.dim + e);
     o[0] = fmaf(g, v.x, o[0]);
     o[1] = fmaf(g, v.y, o[1]);
   }
-  if (wave > 0) {
-    sums[wave - 1][e] = o[0];
-    sums[wave - 1][e + 1] = o[1];
-  }
-  __syncthreads();
-  if (wave > 0) return;
+  if constexpr (W > 1) {
+    if (wave > 0) {
+      sums[wave - 1][e] = o[0];
+      sums[wave - 1][e + 1] = o[1];
+    }
+    __syncthreads();
+    if (wave > 0) return;
 #pragma unroll
-  for (int v = 0; v < 3; ++v) {
-    o[0] += sums[v][e];
-    o[1] += sums[v][e + 1];
+    for (int v = 0; v < W - 1; ++v) {
+      o[0] += sums[v][e];
+      o[1] += sums[v][e + 1];
+    }
   }
   const bool any = sum > 0.0f || sum != sum;
   const float inv = any ? 1.0f / sum : 0.0f;
@@ -495,7 +502,11 @@ void launch(const AttentionArgs& a, bool few, hipStream_t s) {
   else hipLaunchKernelGGL((attention_kernel<DP, false>), grid, dim3(256), 0, s, a);
   if (a.splits == 1) return;
   const int64_t n = static_cast<int64_t>(a.heads) * a.tokens_q;
-  hipLaunchKernelGGL(attention_join_kernel, dim3(static_cast<uint32_t>(n)), dim3(256), 0, s, a);
+  if (a.splits > 8)
+    hipLaunchKernelGGL(attention_join_kernel<4>, dim3(static_cast<uint32_t>(n)), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(attention_join_kernel<1>, dim3(static_cast<uint32_t>((n + 3) / 4)), dim3(256),
+                       0, s, a);
 }
 
 }  // namespace
