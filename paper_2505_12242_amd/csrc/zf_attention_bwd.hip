@@ -168,7 +168,7 @@ struct Shared {
   typedef Heads<DP> H;
   static constexpr int kTile = kRows * H::kPitch;
   static constexpr int kSlot = 2 * kTile + 1024;  // q, dout, lse and delta (256 bytes a wave)
-  static constexpr int kOwn = 2 * kSlot;          // of a group
+  static constexpr int kOwn = (WK == 1 ? 1 : 2) * kSlot;  // of a group
   static constexpr int kValues = WR * kOwn;       // the block's v
   static constexpr int kAll = kValues + 32 * WK * H::kPitch;
   static constexpr int kSums = (WR - 1) * WK * H::kTiles * 4096;
@@ -196,7 +196,8 @@ __global__ __launch_bounds__(64 * WK * WR, 2) void attention_dkv_kernel(Attentio
   {
     const rsrc_t rv = make_rsrc(
         a.v.p + (static_cast<int64_t>(w.k0) + w.first) * a.v.ld_token + kvh * a.v.ld_head, -1);
-    constexpr int kN = 32 / H::kPer / WR;
+    constexpr int kN = 32 / H::kPer / WR > 0 ? 32 / H::kPer / WR : 1;
+    if (wave * kN * H::kPer < 32 * WK)
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
       const int r = (wave * kN + n) * H::kPer + lane / H::kUnits;
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(64 * WK * WR, 2) void attention_dkv_kernel(Attentio
   for (int32_t r0 = begin; r0 < end; r0 += kStep) {
     if (WK == 1) wait_own_dma<0>();
     else wait_dma<0>();
-    if (r0 + kStep < w.rows) load(r0 + kStep, slot ^ 1);
+    if (WK != 1 && r0 + kStep < w.rows) load(r0 + kStep, slot ^ 1);
     const uint32_t q = lane_r + own * kOwn + slot * kSlot, qt = lane_c + own * kOwn + slot * kSlot;
     const uint32_t dout = q + kTile, dout_t = qt + kTile, v = lane_r + kValues + part * 32 * H::kPitch;
     const float* const stats =
@@ -326,7 +327,12 @@ __global__ __launch_bounds__(64 * WK * WR, 2) void attention_dkv_kernel(Attentio
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_setprio(0);
     }
-    slot ^= 1;
+    if (WK == 1) {
+      wait_reads();
+      if (r0 + kStep < w.rows) load(r0 + kStep, 0);
+    } else {
+      slot ^= 1;
+    }
   }
   uint16_t* const to_k = a.dk.p + token * a.dk.ld_token + kvh * a.dk.ld_head;
   uint16_t* const to_v = a.dv.p + token * a.dv.ld_token + kvh * a.dv.ld_head;
@@ -362,16 +368,23 @@ __global__ __launch_bounds__(64 * WK * WR, 2) void attention_dkv_kernel(Attentio
 }
 
 // Forms by the number of blocks of 128 keys (of 512 that the chip holds at once).
-// Few: blocks of 32 keys, a wave's walk a quarter as long (5 sequences of some 500 x
-// 4 key heads 95 us, not 214; 4 x 1024 x 12 heads 60.8, two groups 63.5).  Causal, up
-// to two rounds: the first keys' blocks would be the last to end, so two groups of
-// waves share a walk (8192 x 8 key heads 1940 us, one group 2400; whole 485, not 466).
-// Else one group, without the second one's barriers (2 x 4096 x 32 heads 993, not 1046).
-enum { kNarrow, kTwoGroups, kWide };
-constexpr int64_t kFewBlocks = 448, kTwoRounds = 1024;
+// Few: blocks of 32 keys, whose waves share the walk.  Of these eight waves a block
+// where all of them are on the chip at once, more or less, and long enough, else four
+// (5 sequences of some 500 x 4 key heads x 5: 85 us, with four 102; 4 x 1024 x 12
+// heads 54, with eight 81; 4096 x 8 key heads x 4 534 and 558; one group of waves and
+// 128 keys a block 214 us for the first).  Causal, up to two rounds: the first keys'
+// blocks would be the last to end, so two groups of waves share a walk (8192 x 8 key
+// heads 1940 us, one group 2400; whole 485, not 466).  Else one group, without the
+// second one's barriers (2 x 4096 x 32 heads 993, not 1046).
+enum { kNarrow, kNarrowLong, kTwoGroups, kWide };
+constexpr int64_t kFewBlocks = 448, kTwoRounds = 1024, kLongRows = 1536;
 int32_t form_of(const AttentionBwdArgs& a) {
   const int64_t blocks = ((a.tokens_k >> kLg) + a.sequences) * a.kv_heads;
-  if (blocks < kFewBlocks) return kNarrow;
+  if (blocks < kFewBlocks)
+    return ((a.tokens_k >> 5) + a.sequences) * a.kv_heads <= 512 &&
+                   a.tokens_q * a.group >= kLongRows * a.sequences
+               ? kNarrowLong
+               : kNarrow;
   return a.causal && blocks < kTwoRounds ? kTwoGroups : kWide;
 }
 
@@ -391,6 +404,7 @@ void launch(const AttentionBwdArgs& a, hipStream_t s) {
   if (a.tokens_k == 0) return;
   const int32_t form = form_of(a);
   if (form == kNarrow) launch_dkv<DP, 1, 4>(a, s);
+  else if (form == kNarrowLong) launch_dkv<DP, 1, 8>(a, s);
   else if (form == kTwoGroups) launch_dkv<DP, 4, 2>(a, s);
   else launch_dkv<DP, 4, 1>(a, s);
 }
@@ -406,7 +420,7 @@ hipError_t launch_attention_backward(AttentionBwdArgs a, void* ws, hipStream_t s
   a.delta = static_cast<float*>(ws);
   a.tiles = static_cast<int32_t>((a.tokens_q * a.group >> kLg) + a.sequences);
   a.key_tiles =
-      static_cast<int32_t>((a.tokens_k >> (form_of(a) == kNarrow ? 5 : kLg)) + a.sequences);
+      static_cast<int32_t>((a.tokens_k >> (form_of(a) <= kNarrowLong ? 5 : kLg)) + a.sequences);
   if (a.dim <= 64) launch<64>(a, s);
   else if (a.dim <= 96) launch<96>(a, s);
   else launch<128>(a, s);
