@@ -128,7 +128,10 @@ CASES = [
     dict(lens=[(90, 150)], heads=2, dim=128, std=6.0),       # scores of some hundreds
     dict(lens=[(200, 200)], heads=2, dim=64, scale=1e-3),
     dict(lens=[(31, 2000)], heads=4, kv=2, dim=128),
-    # gradients by blocks of 128 keys, one group of waves or two
+    # gradients by blocks of 32 keys, eight waves each
+    dict(lens=[(420, 300)], heads=4, dim=96),
+    dict(lens=[(800, 800), (17, 40)], heads=4, kv=1, dim=40),
+    # by blocks of 128 keys, one group of waves or two
     dict(lens=[(150, 200), (260, 260), (33, 190)] * 3, heads=32, kv=32, dim=72),
     dict(lens=[(150, 200), (260, 260), (33, 190)] * 3, heads=32, kv=32, dim=128, causal=False),
     dict(lens=[(150, 200), (260, 260), (70, 190)] * 3, heads=40, kv=20, dim=64),
