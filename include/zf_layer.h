@@ -232,7 +232,8 @@ zf_status zf_linear_fp8_backward(const void* dy, int64_t ld_dy, const void* z, i
 
 /* HOST struct of a DEVICE pointer: bf16 vectors of `dim` elements, one for each
  * token and head, at data + token * ld_token + head * ld_head (elements).
- * data is 16-byte aligned, both strides are multiples of 8 and below 2^23. */
+ * data is 16-byte aligned; both strides are multiples of 8, ld_token below 2^23
+ * and ld_head below 2^40. */
 typedef struct zf_heads {
   void* data;
   int64_t ld_token;

@@ -59,8 +59,9 @@ __device__ __forceinline__ float slope(float z) {
     return fmaf(z * 0.3989422804014327f, e, phi);  // 1 / sqrt(2 pi)
   }
   if constexpr (ACT == ZF_GELU_TANH) {
-    const float p = tanh_phi(z);
-    return fmaf(z * p * (1.0f - p), 2.0f * kTanhScale * fmaf(0.134145f * z, z, 1.0f), p);
+    const float p = tanh_phi(z), w = p * (1.0f - p);
+    // (where w is 0 the other factor may be infinite)
+    return w == 0.0f ? p : fmaf(z * w, 2.0f * kTanhScale * fmaf(0.134145f * z, z, 1.0f), p);
   }
   if constexpr (ACT == ZF_SILU) {
     const float p = __builtin_amdgcn_rcpf(1.0f + exp_neg(z));

@@ -28,9 +28,10 @@ struct Rows {
   int32_t lim;   // keys that the lane's row sees
 };
 
-// A weight of 0 hides no infinity and no NaN from a product.  So where some row does
-// not see keys that others do, such elements of v become zeros in LDS, before the
-// product, and are added behind the loop, to the rows that see them (add_odd).
+// A weight of 0 hides no infinity and no NaN from a product.  So in the tiles with
+// weights of 0, where some row does not see keys that others do, or behind the last
+// key, such elements of v become zeros in LDS, before the product, and are added
+// behind the loop, to the rows that see them (add_odd).
 
 // The halves of a word whose exponent is all ones, as 0x8000 each.
 __device__ __forceinline__ uint32_t odd_halves(uint32_t x) {
@@ -264,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     if (kb + kKeys < end)
       keys.template load<true, true>(kb + kKeys, base + (slot ^ 1) * 2 * kTile, wave);
     const uint32_t in = base + slot * 2 * kTile;
-    if (mask.value && whole < w.lk)
+    if (mask.value)
       odd |= __syncthreads_or(scrub<kTile / 4096>(in + kTile + wave * (kTile / 4)));
     if (kb < most)
       tile_step<DP, kKeys, mask.value>(x, in + rows, in + kTile + columns, kb, a.scale * kLog2E,
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few_kernel(Attent
           [&] {
             if (next) wait_own_dma<kN>();
             else wait_own_dma<0>();
-            if (mask.value && least < w.lk) odd |= scrub<S::kTile / 1024>(base + kTile);
+            if (mask.value) odd |= scrub<S::kTile / 1024>(base + kTile);
           });
       wait_reads();
       if (next) keys.template load<false, true>(kb + kFewStep, base + kTile, 0);

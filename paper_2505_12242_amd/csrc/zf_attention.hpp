@@ -249,11 +249,11 @@ __device__ __forceinline__ void pin(v16f (&x)[N]) {
   for (int t = 0; t < N; ++t) asm volatile("" : "+v"(x[t]));
 #endif
 }
-// Waits until at most N of the wave's loads are in flight, then for the block's
-// other waves.
+// Waits until at most N of the wave's loads are in flight and its reads of LDS are
+// done (the other waves may load where it read), then for the block's other waves.
 template <int N>
 __device__ __forceinline__ void wait_dma() {
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 // The same without the other waves.

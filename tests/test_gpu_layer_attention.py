@@ -288,6 +288,26 @@ def test_hidden_keys_reach_nothing(lens, heads, kv, dim, value, which):
         assert torch.equal(got.out[d.qs[1]:d.qs[-1]], want.out[d.qs[1]:d.qs[-1]])
 
 
+@pytest.mark.parametrize("lens,heads,kv,dim,causal", [([(90, 70), (5, 131)], 2, 1, 64, False),
+                                                      ([(1, 45), (1, 300)], 8, 2, 128, True),
+                                                      ([(3, 50)], 4, 1, 96, False)])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")])
+def test_an_infinity_that_every_query_sees(lens, heads, kv, dim, causal, value):
+    """In the last key's v, whose copies fill its tile: the sum is that infinity, as the
+    weight of the key is positive (no score is farther than exp(-60) from another)."""
+    c = Case(lens, heads, kv, dim, causal)
+    want = c.run()
+    for i, (_, lk) in enumerate(lens):
+        d = Case(lens, heads, kv, dim, causal)
+        d.gv[d.ks[i] + lk - 1, 0, 5] = value
+        got = d.run()
+        rows = slice(d.qs[i], d.qs[i + 1])
+        assert (got.out[rows, :heads // kv, 5] == value).all()
+        got.out[rows, :heads // kv, 5] = want.out[rows, :heads // kv, 5]
+        m = slice(d.qs[0], d.qs[-1])
+        assert torch.equal(got.out[m], want.out[m])
+
+
 def test_captured_call_follows_the_lengths():
     c = Case([(1, 700), (1, 20), (1, 0)], 8, 2, 128, room=1024)
     stream = torch.cuda.Stream()

@@ -153,6 +153,21 @@ def test_activation_over_its_range(name):
     assert torch.equal(got.dz[0], got.dbias)
 
 
+@pytest.mark.parametrize("name", ACTS[1:])
+def test_activation_of_large_values(name):
+    """Every finite bf16 number beyond 2^12: value and slope are z and 1, or 0 (the
+    exponentials there are 0 in 32 bits and their complements 1)."""
+    z = torch.arange(0, 65536, dtype=torch.int32).to(torch.int16).view(BF16).float()
+    z = z[torch.isfinite(z) & (z.abs() > 4096)]
+    n = z.numel()
+    a, _ = random_fp8(zf, 1, 0, 1, torch.Generator().manual_seed(1))
+    y = zf.linear_fp8(a, zf.alloc_fp8(n, 0), z.cuda(), name, dtype=F32).y[0].cpu()
+    assert torch.equal(y, z.clamp(min=0))
+    got = zf.linear_fp8_backward(torch.ones(1, n, device="cuda"), z[None].cuda(), name, rows=False,
+                                 transposed=False, want_dz=True)
+    assert torch.equal(got.dz[0].cpu(), (z > 0).float())
+
+
 BACK = [(1, 1), (5, 300), (16, 128), (127, 129), (128, 256), (300, 515), (1000, 264), (129, 2048)]
 
 
