@@ -7,7 +7,8 @@
 // walks the rows that see them, over all query heads of the key head: scores, dP,
 // dk and dv.  Seven products in place of the five that one kernel needs, but no
 // gradient is summed across blocks: no atomics, no partial results in memory, and
-// the same bits on every run.
+// the same bits on every run.  2 x 4096 tokens x 32 heads of 128, causal: 400 us and
+// 550, 1.0 PFLOP/s of these products either (the library's 8192^3 bf16 product 1.26).
 //
 // In either, the operand that a wave keeps (rows, or keys) stays in registers and
 // runs along the lanes of the scores; what is walked runs along their registers,

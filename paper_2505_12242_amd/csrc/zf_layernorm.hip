@@ -6,7 +6,9 @@
 // fp32.  The squares are summed about the mean, in a second pass over the
 // registers and a second barrier: nothing cancels, as a sum of squares less a
 // squared sum would.  (Each wave's squares about its own mean, joined with one
-// barrier, cost more than the barrier: 8192 x 5120 bf16 144 us.)
+// barrier, cost more than the barrier: 8192 x 5120 bf16 144 us.)  Bound by HBM:
+// 8192 x 5120 bf16 with a residual, h, y and 8 bits, 378 MB in 71 us, 5.3 TB/s, 0.79
+// of a copy's rate.
 #include <algorithm>
 
 #include "zf_norm.hpp"
@@ -171,8 +173,12 @@ __device__ __forceinline__ float2 block_sum2(float x, float y, float2 (&red)[NT 
   return s;
 }
 
-// GRADS: the gain's and the bias's partial sums are kept (the bias's behind all
-// blocks' of the gain).
+// A block takes rows one after the other, the next one's loads in flight where a
+// thread has one piece, and keeps its columns' sums for both gradients in registers.
+// 8192 x 5120 bf16 with a residual: 336 MB and the partial sums in 69 us, 4.9 TB/s, and 5
+// us to join those; bound by HBM through few loads in flight (the sums' registers leave
+// a CU few waves).  GRADS: the gain's and the bias's partial sums are kept (the bias's
+// behind all blocks' of the gain).
 template <typename T, int NT, int V, bool DRES, bool GRADS>
 __global__ __launch_bounds__(NT) void layernorm_backward_kernel(LayerNormBwdArgs a) {
   __shared__ float2 red[2][NT / 64];

@@ -5,6 +5,10 @@
 // Tiles and blocks as the quantiser's (zf_fp8.hip), whose 8-bit copies these
 // are.  The bias's gradient is summed before rounding: over a thread's 8 rows,
 // the tile's other 15 units of rows, and, in tile order, by a second kernel.
+//
+// 4096 x 11008 bf16 with an activation: 271 MB in 62 us, 4.4 TB/s (plus 4 to join the
+// bias's sums): as for the quantiser, a tile's loads, reductions and stores follow one
+// another and only other blocks overlap them.
 #include "zf_activation.hpp"
 #include "zf_norm.hpp"
 #include "zf_quantize.hpp"

@@ -11,6 +11,11 @@
 // tiles: the reduction is split over blocks and the shares' results joined in order
 // (64 x 11008 x 4096: 22 + 4 us).  Up to 16 rows: the second operand's bytes are all
 // that counts (matmul_rows_kernel; 1 x 11008 x 4096: 45 MB in 11.8 us, 3.8 TB/s).
+//
+// What follows the product in a linear layer (bias, activation, residual, 8 bits) is
+// done on the fp32 sums while they pass through LDS on their way out, or by the
+// kernel that joins the shares: 4096 x 11008 x 4096 353 us with all of it, the product
+// alone 318 to 352 (by the card's clock); 8 x 11008 x 4096 to 8 bits 18.6 us.
 #include <algorithm>
 
 #include "zf_activation.hpp"

@@ -256,3 +256,26 @@ def test_binding_layer():
         zf.linear_fp8_backward(x[:0], None, "gelu")
     with pytest.raises(ValueError):
         zf.linear_fp8_backward(x[:0], rows=False, transposed=False, want_dbias=False)
+
+
+def test_tensors_of_other_gpus():
+    """With more than one GPU: all tensors on the launch's."""
+    class On:
+        is_cuda = True
+
+        def __init__(self, i):
+            self.index = i
+
+        def get_device(self):
+            return self.index
+
+    class Stream:
+        def __init__(self, i):
+            self.device = torch.device("cuda", i)
+
+    host = torch.zeros(1)
+    _lib._same_device(Stream(1), q=On(1), k=None, v=host, out=On(1))
+    with pytest.raises(ValueError, match="^k: lives on GPU 0, other arguments on GPU 1"):
+        _lib._same_device(Stream(1), q=On(1), k=On(0))
+    with pytest.raises(ValueError, match="^k: lives on GPU 1, the call is launched on GPU 0"):
+        _lib._same_device(Stream(0), q=None, k=On(1))

@@ -288,6 +288,21 @@ def test_hidden_keys_reach_nothing(lens, heads, kv, dim, value, which):
         assert torch.equal(got.out[d.qs[1]:d.qs[-1]], want.out[d.qs[1]:d.qs[-1]])
 
 
+@pytest.mark.parametrize("lens,heads,kv", [([(128, 300)], 2, 2), ([(40, 40)], 4, 1), ([(4, 300)], 2, 1)])
+def test_hidden_scores_round_nothing(lens, heads, kv):
+    """Keys of large scores, seen by the last queries alone: the others' results keep
+    their bits."""
+    c, d = Case(lens, heads, kv, 64, behind=0), Case(lens, heads, kv, 64, behind=0)
+    lq, lk = lens[0]
+    half = lq // 2
+    d.gk[d.ks[0] + lk - half:] *= 64.0
+    want, got = c.run(), d.run()
+    rows = slice(c.qs[0], c.qs[0] + lq - half)
+    assert torch.equal(got.out[rows], want.out[rows])
+    assert torch.equal(got.lse[:, rows], want.lse[:, rows])
+    assert not torch.equal(got.out, want.out)
+
+
 @pytest.mark.parametrize("lens,heads,kv,dim,causal", [([(90, 70), (5, 131)], 2, 1, 64, False),
                                                       ([(1, 45), (1, 300)], 8, 2, 128, True),
                                                       ([(3, 50)], 4, 1, 96, False)])
