@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64 * WK * WR, 2) void attention_dkv_kernel(Attentio
 // Forms by the number of blocks of 128 keys (of 512 that the chip holds at once).
 // Few: blocks of 32 keys, whose waves share the walk.  Of these eight waves a block
 // where all of them are on the chip at once, more or less, and long enough, else four
-// (5 sequences of some 500 x 4 key heads x 5: 85 us, with four 102; 4 x 1024 x 12
+// (11 sequences of 1 to 1003 x 4 key heads x 5: 85 us, with four 102; 4 x 1024 x 12
 // heads 54, with eight 81; 4096 x 8 key heads x 4 534 and 558; one group of waves and
 // 128 keys a block 214 us for the first).  Causal, up to two rounds: the first keys'
 // blocks would be the last to end, so two groups of waves share a walk (8192 x 8 key
