@@ -1,9 +1,9 @@
 // Attention's gradients (formulas and contract in zf_layer.h; rows, products and
 // the layout of LDS in zf_attention.hpp).
 //
-// Two kernels.  The first takes 128 rows a block, as the forward pass does, and
-// walks their keys: scores again, dP, dS, dq; before that it forms d = dout . out
-// of its rows, which the second needs too.  The second takes 128 keys a block and
+// Two kernels.  The first takes 128 rows a block, as the forward pass does (or 32,
+// where there are few), and walks their keys: scores again, dP, dS, dq; before that
+// it forms d = dout . out of its rows, which the second needs too.  The second takes 128 keys a block and
 // walks the rows that see them, over all query heads of the key head: scores, dP,
 // dk and dv.  Seven products in place of the five that one kernel needs, but no
 // gradient is summed across blocks: no atomics, no partial results in memory, and
@@ -69,6 +69,37 @@ __device__ __forceinline__ void store_vector(uint16_t* p, int dim, const v16f (&
   for (int t = 0; t < DP / 32; ++t) store_tile(p, dim, t, x[t], scale);
 }
 
+// A wave's 32 rows, a row a lane.
+template <int DP>
+struct Rows {
+  v8b q[DP / 16], dout[DP / 16];
+  v16f dq[DP / 32];
+  float delta, lse;  // (lse in powers of two)
+};
+template <int DP>
+__device__ __forceinline__ void load_rows(const AttentionBwdArgs& a, int64_t token, int64_t head,
+                                          Rows<DP>& x) {
+  load_vector<DP>(a.q.p + token * a.q.ld_token + head * a.q.ld_head, a.dim, x.q);
+  load_vector<DP>(a.dout.p + token * a.dout.ld_token + head * a.dout.ld_head, a.dim, x.dout);
+  v8b out[DP / 16];
+  load_vector<DP>(a.out.p + token * a.out.ld_token + head * a.out.ld_head, a.dim, out);
+  x.lse = a.lse[head * a.tokens_q + token] * kLog2E;
+  x.delta = 0.0f;
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      x.delta = fmaf(static_cast<float>(x.dout[c][e]), static_cast<float>(out[c][e]), x.delta);
+  x.delta += other_half(x.delta);
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t) x.dq[t] = zero16();
+  settle(x.q);
+  settle(x.dout);
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(x.lse));  // (see settle)
+#endif
+}
+
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a) {
   typedef Heads<DP> H;
@@ -84,30 +115,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
   const int32_t i = min(row, w.rows - 1) / a.group;
   const int64_t head = kvh * a.group + min(row, w.rows - 1) - i * a.group;
   const int64_t token = w.q0 + i;
-  v8b q[H::kChunks], dout[H::kChunks];
-  load_vector<DP>(a.q.p + token * a.q.ld_token + head * a.q.ld_head, a.dim, q);
-  load_vector<DP>(a.dout.p + token * a.dout.ld_token + head * a.dout.ld_head, a.dim, dout);
-  float delta = 0.0f;
-  {
-    v8b out[H::kChunks];
-    load_vector<DP>(a.out.p + token * a.out.ld_token + head * a.out.ld_head, a.dim, out);
-#pragma unroll
-    for (int c = 0; c < H::kChunks; ++c)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        delta = fmaf(static_cast<float>(dout[c][e]), static_cast<float>(out[c][e]), delta);
-    delta += other_half(delta);
-  }
-  if (valid && lane < 32) a.delta[head * a.tokens_q + token] = delta;
-  float lse = a.lse[head * a.tokens_q + token] * kLog2E;
-#ifdef __HIP_DEVICE_COMPILE__
-  asm volatile("" : "+v"(lse));  // (see settle)
-#endif
   const float c = a.scale * kLog2E;
   const int32_t lim = keys_of(a, w, i);
-  v16f acc[H::kTiles];
-#pragma unroll
-  for (int t = 0; t < H::kTiles; ++t) acc[t] = zero16();
 
   const auto token_of = [&](int32_t row) { return min(row, w.rows - 1) / a.group; };
   const int32_t least = uniform_i32(keys_of(a, w, token_of(w.first + 32 * wave)));
@@ -117,8 +126,9 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
   const KeyLoader<DP, kKeys, 4> keys(a, w, kvh, wave);
   const uint32_t base = lds_offset(lds), rows = H::lane_rows(), columns = H::lane_columns();
   if (end > 0) keys.template load<true, true>(0, base, wave);
-  settle(q);
-  settle(dout);
+  Rows<DP> x;
+  load_rows(a, token, head, x);
+  if (valid && lane < 32) a.delta[head * a.tokens_q + token] = x.delta;
   int slot = 0;
   for (int32_t kb = 0; kb < end; kb += kKeys) {
     wait_dma<0>();
@@ -131,12 +141,12 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
       for (int t = 0; t < 2; ++t) {
         v16f s = zero16(), dp = zero16();
 #pragma unroll
-        for (int j = 0; j < H::kChunks; ++j) s = mma(H::frag(k, 32 * t, j), q[j], s);
+        for (int j = 0; j < H::kChunks; ++j) s = mma(H::frag(k, 32 * t, j), x.q[j], s);
 #pragma unroll
-        for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(v, 32 * t, j), dout[j], dp);
+        for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(v, 32 * t, j), x.dout[j], dp);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse)) * (dp[r] - delta);
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -x.lse)) * (dp[r] - x.delta);
         if (mask) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
@@ -147,14 +157,104 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBwdArgs a
           const v8b ds = pack8(s, j);
 #pragma unroll
           for (int u = 0; u < H::kTiles; ++u)
-            acc[u] = mma(H::frag_t(kt, 32 * t + 16 * j, u), ds, acc[u]);
+            x.dq[u] = mma(H::frag_t(kt, 32 * t + 16 * j, u), ds, x.dq[u]);
         }
       }
     }
     slot ^= 1;
   }
   if (valid)
-    store_vector<DP>(a.dq.p + token * a.dq.ld_token + head * a.dq.ld_head, a.dim, acc, a.scale);
+    store_vector<DP>(a.dq.p + token * a.dq.ld_token + head * a.dq.ld_head, a.dim, x.dq, a.scale);
+}
+
+// The same for few rows: 32 of them a block, which all of its waves keep, and every
+// fourth tile of 32 keys a wave, loaded by it for itself; their sums are added in LDS,
+// in the waves' order.  v's slot is filled again as soon as dP is done, k's after dq.
+constexpr int kDqWaves = 4, kDqStep = 32 * kDqWaves;
+template <int DP>
+__global__ __launch_bounds__(64 * kDqWaves, 2) void attention_dq_narrow_kernel(AttentionBwdArgs a) {
+  typedef Heads<DP> H;
+  typedef KeyLoader<DP, 32, 1> Loader;
+  constexpr int kTile = 32 * H::kPitch, kN = Loader::kLoads;
+  static_assert(kDqWaves * 2 * kTile >= (kDqWaves - 1) * H::kTiles * 4096, "the sums fit the tiles");
+  __shared__ __align__(1024) uint8_t lds[kDqWaves * 2 * kTile];
+  const int lane = threadIdx.x & 63, wave = uniform_i32(threadIdx.x >> 6), half = lane >> 5;
+  const int32_t kvh = blockIdx.x % a.kv_heads;
+  Sequence w;
+  if (!find_tile<false>(a, a.tiles - 1 - static_cast<int64_t>(blockIdx.x / a.kv_heads), 5, w)) return;
+  const int32_t row = w.first + (lane & 31);
+  const bool valid = row < w.rows;
+  const int32_t i = min(row, w.rows - 1) / a.group;
+  const int64_t head = kvh * a.group + min(row, w.rows - 1) - i * a.group;
+  const int64_t token = w.q0 + i;
+  const int32_t lim = keys_of(a, w, i);
+  const int32_t least = uniform_i32(keys_of(a, w, w.first / a.group));
+  const int32_t end = uniform_i32(keys_of(a, w, min(w.first + 31, w.rows - 1) / a.group));
+  const Loader keys(a, w, kvh, 0);
+  const uint32_t base = lds_offset(lds) + wave * 2 * kTile;
+  const int32_t first = 32 * wave;
+  if (first < end) {
+    keys.template load<false, true>(first, base + kTile, 0);
+    keys.template load<true, false>(first, base, 0);
+  }
+  Rows<DP> x;
+  load_rows(a, token, head, x);
+  if (valid && wave == 0 && lane < 32) a.delta[head * a.tokens_q + token] = x.delta;
+  const float c = a.scale * kLog2E;
+  const uint32_t k = base + H::lane_rows(), kt = base + H::lane_columns(), v = k + kTile;
+  for (int32_t kb = first; kb < end; kb += kDqStep) {
+    const bool next = kb + kDqStep < end;
+    wait_own_dma<kN>();  // (this k is behind this v)
+    v16f s = zero16(), dp = zero16();
+#pragma unroll
+    for (int j = 0; j < H::kChunks; ++j) dp = mma(H::frag(v, 0, j), x.dout[j], dp);
+    wait_reads();
+    if (next) {
+      keys.template load<false, true>(kb + kDqStep, base + kTile, 0);
+      wait_own_dma<kN>();
+    } else {
+      wait_own_dma<0>();
+    }
+#pragma unroll
+    for (int j = 0; j < H::kChunks; ++j) s = mma(H::frag(k, 0, j), x.q[j], s);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -x.lse)) * (dp[r] - x.delta);
+    if (kb + 32 > least) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (kb + reg_row(r) + 4 * half >= lim) s[r] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const v8b ds = pack8(s, j);
+#pragma unroll
+      for (int u = 0; u < H::kTiles; ++u) x.dq[u] = mma(H::frag_t(kt, 16 * j, u), ds, x.dq[u]);
+    }
+    wait_reads();
+    if (next) keys.template load<true, false>(kb + kDqStep, base, 0);
+    pin(x.dq);
+  }
+  // (a wave waits for its last tile's loads)
+  float* const sums = reinterpret_cast<float*>(lds);
+  const auto place = [&](int wave, int t, int r) {
+    return sums + (((wave - 1) * H::kTiles + t) * 16 + r) * 64 + lane;
+  };
+  __syncthreads();
+  if (wave > 0)
+#pragma unroll
+    for (int t = 0; t < H::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) *place(wave, t, r) = x.dq[t][r];
+  __syncthreads();
+  if (wave > 0 || !valid) return;
+#pragma unroll
+  for (int g = 1; g < kDqWaves; ++g)
+#pragma unroll
+    for (int t = 0; t < H::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x.dq[t][r] += *place(g, t, r);
+  store_vector<DP>(a.dq.p + token * a.dq.ld_token + head * a.dq.ld_head, a.dim, x.dq, a.scale);
 }
 
 // 32 WK keys a block, of which a wave keeps 32: k in registers, v in LDS.  WR groups
@@ -389,6 +489,13 @@ int32_t form_of(const AttentionBwdArgs& a) {
   return a.causal && blocks < kTwoRounds ? kTwoGroups : kWide;
 }
 
+int64_t row_tiles(const AttentionBwdArgs& a, int lg) { return (a.tokens_q * a.group >> lg) + a.sequences; }
+// dq by blocks of 32 rows where those of 128 are fewer than the CUs, and a walk's length is
+// what counts (both gradients, 132 blocks: 4096 tokens x 4 heads 110 us, with 128 rows
+// 172; 144: 1024 x 16 heads 42, 56; 288: 1024 x 32 heads 72.7, 73.8; 272: 2 x 512 x 8 key
+// heads x 4 57.8, 53.9; 620: the first of the above 92, 85).
+bool dq_narrow(const AttentionBwdArgs& a) { return row_tiles(a, kLg) * a.kv_heads <= 256; }
+
 template <int DP, int WK, int WR>
 void launch_dkv(const AttentionBwdArgs& a, hipStream_t s) {
   constexpr int kBytes = Shared<DP, WK, WR>::kBytes;
@@ -399,7 +506,10 @@ void launch_dkv(const AttentionBwdArgs& a, hipStream_t s) {
 
 template <int DP>
 void launch(const AttentionBwdArgs& a, hipStream_t s) {
-  if (a.tokens_q > 0)
+  if (a.tokens_q > 0 && dq_narrow(a))
+    hipLaunchKernelGGL((attention_dq_narrow_kernel<DP>),
+                       dim3(static_cast<uint32_t>(a.tiles) * a.kv_heads), dim3(64 * kDqWaves), 0, s, a);
+  else if (a.tokens_q > 0)
     hipLaunchKernelGGL((attention_dq_kernel<DP>), dim3(static_cast<uint32_t>(a.tiles) * a.kv_heads),
                        dim3(256), 0, s, a);
   if (a.tokens_k == 0) return;
@@ -419,7 +529,7 @@ size_t attention_backward_workspace(const AttentionBwdArgs& a) {
 hipError_t launch_attention_backward(AttentionBwdArgs a, void* ws, hipStream_t s) {
   (void)hipGetLastError();
   a.delta = static_cast<float*>(ws);
-  a.tiles = static_cast<int32_t>((a.tokens_q * a.group >> kLg) + a.sequences);
+  a.tiles = static_cast<int32_t>(row_tiles(a, dq_narrow(a) ? 5 : kLg));
   a.key_tiles =
       static_cast<int32_t>((a.tokens_k >> (form_of(a) <= kNarrowLong ? 5 : kLg)) + a.sequences);
   if (a.dim <= 64) launch<64>(a, s);
