@@ -202,6 +202,32 @@ def test_starts_outside_the_tensors_are_cut_off(starts_q, starts_k):
     assert torch.equal(got.out, want.out) and torch.equal(got.lse, want.lse)
 
 
+@pytest.mark.parametrize("far", ["tokens", "heads"])
+def test_offsets_beyond_32_bits(far):
+    """Vectors more than 2^32 bytes apart, of tokens or of heads."""
+    c = Case([(130, 260), (1, 30)], heads=2, kv=2 if far == "heads" else 1, ahead=0, behind=0)
+    token, head = ((1 << 23) - 64, 64) if far == "tokens" else (64, (1 << 31) + 64)
+
+    def spread(buf, shape, column=0):
+        return buf.as_strided((*shape[:2], 64), (token, head, 1), column)
+
+    column = 1024 if far == "tokens" else 64 * 512
+    size = (c.k.shape[0] - 1) * token + (c.heads - 1) * head + 4 * column
+    bufs = [torch.empty(size, dtype=BF16, device="cuda") for _ in range(5)]
+    q, k, v, do = (spread(bufs[0], t.shape, i * column).copy_(t)
+                   for i, t in enumerate((c.q, c.k, c.v, c.do)))
+    got = zf.attention(q, k, v, c.seq_q, c.seq_k, scale=c.scale, out=spread(bufs[1], q.shape),
+                       want_lse=True)
+    check_forward(c, got.out, got.lse)
+    # (single tokens, by pieces of keys)
+    near = [t.contiguous() for t in (q[:1], k, v)]
+    assert torch.equal(zf.attention(q[:1], k, v).out, zf.attention(*near).out)
+    dq, dk, dv = (spread(b, t.shape) for b, t in zip(bufs[2:], (q, k, v)))
+    grads = zf.attention_backward(do, q, k, v, *got, c.seq_q, c.seq_k, scale=c.scale, dq=dq, dk=dk,
+                                  dv=dv)
+    check_backward(c, *got, grads)
+
+
 def test_no_tokens():
     q, k = torch.zeros(0, 4, 64, dtype=BF16, device="cuda"), torch.zeros(5, 2, 64, dtype=BF16, device="cuda")
     assert zf.attention(q, k, k, ints([0, 0]), ints([0, 5])).out.shape == (0, 4, 64)
