@@ -7,7 +7,7 @@
 // registers and a second barrier: nothing cancels, as a sum of squares less a
 // squared sum would.  (Each wave's squares about its own mean, joined with one
 // barrier, cost more than the barrier: 8192 x 5120 bf16 144 us.)  Bound by HBM:
-// 8192 x 5120 bf16 with a residual, h, y and 8 bits, 378 MB in 71 us, 5.3 TB/s, 0.79
+// 8192 x 5120 bf16 with a residual, h, y and 8 bits, 378 MB in 69.5 us, 5.4 TB/s, 0.8
 // of a copy's rate.
 #include <algorithm>
 
@@ -19,15 +19,14 @@ namespace {
 // y of 8 elements written, in its own type and in 8 bits (as the RMS norm's).
 template <typename T>
 __device__ __forceinline__ void store_y(const LayerNormArgs& a, int64_t row, int64_t c,
-                                        const Vec8<T>& h, float mean, float rstd) {
+                                        const Vec8<T>& h, const float (&g)[8], const float (&b)[8],
+                                        float mean, float rstd) {
   const int64_t valid = a.cols - c;
-  float g[8], b[8] = {};
-  load_gain(a, c, g);
-  if (a.bias != nullptr) load_vector(a.bias, a.gain_f32, a.cols, c, b);
+  float o[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) g[j] = j < valid ? ((h[j] - mean) * rstd) * g[j] + b[j] : 0.0f;
+  for (int j = 0; j < 8; ++j) o[j] = j < valid ? ((h[j] - mean) * rstd) * g[j] + b[j] : 0.0f;
   Vec8<T> y;
-  y.set(g);
+  y.set(o);
   if (a.y != nullptr) y.template store<true>(static_cast<T*>(a.y) + row * a.ld_y + c, valid);
   if (a.q.data != nullptr) {
     const uint32_t code = fp8_code(max16(abs_max(y)));
@@ -41,11 +40,23 @@ struct Moments {
   float mean, rstd;
 };
 
+// Keeps a bf16 row packed from one pass over it to the next: unpacked once for all
+// of them, it takes twice the registers.
+template <int V>
+__device__ __forceinline__ void repack(Vec8<uint16_t> (&h)[V]) {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+  for (int i = 0; i < V; ++i) asm volatile("" : "+v"(h[i].u));
+#endif
+}
+template <int V>
+__device__ __forceinline__ void repack(Vec8<float> (&)[V]) {}
+
 // The row's moments in every thread: piece i of V of the thread's 8 elements
 // are columns (threadIdx.x + i * NT) * 8 and on, zeros past the row's end.
 // `red`: two of block_sum's.
 template <typename T, int NT, int V>
-__device__ __forceinline__ Moments moments(const Vec8<T> (&h)[V], int64_t cols, float eps,
+__device__ __forceinline__ Moments moments(Vec8<T> (&h)[V], int64_t cols, float eps,
                                            float (&red)[2][NT / 64]) {
   const float inv = 1.0f / static_cast<float>(cols > 0 ? cols : 1);
   float s = 0.0f;
@@ -54,6 +65,7 @@ __device__ __forceinline__ Moments moments(const Vec8<T> (&h)[V], int64_t cols, 
 #pragma unroll
     for (int j = 0; j < 8; ++j) s += h[i][j];
   const float mean = block_sum<NT>(s, red[0]) * inv;
+  repack(h);
   float m2 = 0.0f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -75,12 +87,17 @@ __device__ __forceinline__ Moments moments(const Vec8<T> (&h)[V], int64_t cols, 
   return Moments{mean, 1.0f / sqrtf(block_sum<NT>(m2, red[1]) * inv + eps)};
 }
 
-template <typename T, int NT, int V, bool RES>
+// G: the gain's and the bias's type.  Beside bf16 rows both are loaded with the row:
+// loads behind the stores of h wait for these too (8192 x 5120 69.5 us, not 71.6; 4096
+// columns without residual and 8 bits 28.8, not 32.5).  Beside fp32 rows they would
+// fill the registers (4096 x 5003 85 us, not 75).
+template <typename T, typename G, int NT, int V, bool RES>
 __global__ __launch_bounds__(NT, V == 1 ? 8 : 1) void layernorm_kernel(LayerNormArgs a) {
   __shared__ float red[2][2][NT / 64];
   int flip = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     Vec8<T> h[V], r[RES ? V : 1];
+    Vec8<G> g[V], b[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8;
@@ -89,9 +106,24 @@ __global__ __launch_bounds__(NT, V == 1 ? 8 : 1) void layernorm_kernel(LayerNorm
         r[i].template fetch<true>(static_cast<const T*>(a.residual) + row * a.ld_residual + c,
                                   a.cols - c);
     }
+    const auto fetch = [&](int i) {
+      const int64_t c = (threadIdx.x + i * NT) * 8;
+      g[i].fetch(static_cast<const G*>(a.gain) + c, a.cols - c);
+      b[i].fetch(static_cast<const G*>(a.bias) + c, a.bias != nullptr ? a.cols - c : 0);
+    };
+    const auto settle = [&](int i) {
+      const int64_t c = (threadIdx.x + i * NT) * 8;
+      g[i].settle(a.cols - c);
+      b[i].settle(a.bias != nullptr ? a.cols - c : 0);
+    };
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) fetch(i);
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int64_t c = (threadIdx.x + i * NT) * 8;
+      if constexpr (sizeof(T) == 2) settle(i);
       h[i].settle(a.cols - c);
       if constexpr (RES) {
         r[i].settle(a.cols - c);
@@ -101,13 +133,26 @@ __global__ __launch_bounds__(NT, V == 1 ? 8 : 1) void layernorm_kernel(LayerNorm
         h[i].template store<true>(static_cast<T*>(a.h) + row * a.ld_h + c, a.cols - c);
     }
     const Moments m = moments<T, NT, V>(h, a.cols, a.eps, red[flip]);
+    repack(h);
     flip ^= 1;
     if (threadIdx.x == 0) {
       a.mean[row] = m.mean;
       a.rstd[row] = m.rstd;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) store_y(a, row, (threadIdx.x + i * NT) * 8, h[i], m.mean, m.rstd);
+    for (int i = 0; i < V; ++i) {
+      if constexpr (sizeof(T) != 2) {
+        fetch(i);
+        settle(i);
+      }
+      float gain[8], bias[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        gain[j] = g[i][j];
+        bias[j] = b[i][j];
+      }
+      store_y(a, row, (threadIdx.x + i * NT) * 8, h[i], gain, bias, m.mean, m.rstd);
+    }
   }
 }
 
@@ -151,7 +196,10 @@ __global__ __launch_bounds__(NT) void layernorm_wide_kernel(LayerNormArgs a) {
       load_h(c);  // (before h, which may be x's or the residual's own buffer, is written)
       if (a.residual != nullptr || (a.h != nullptr && a.h != a.x))
         h.store(static_cast<T*>(a.h) + row * a.ld_h + c, a.cols - c);
-      store_y(a, row, c, h, mean, rstd);
+      float g[8], b[8] = {};
+      load_gain(a, c, g);
+      if (a.bias != nullptr) load_vector(a.bias, a.gain_f32, a.cols, c, b);
+      store_y(a, row, c, h, g, b, mean, rstd);
     }
   }
 }
@@ -349,7 +397,7 @@ int64_t backward_blocks(int64_t rows, int64_t cols) {
 
 // f(threads, pieces a thread) of the forward pass: bf16 rows of more than 2048 columns
 // in blocks of 256 threads with more pieces each, which wait for fewer waves at a
-// barrier (8192 x 5120 71 us, 82 with one piece; 8192 x 8192 109, not 114; fp32 81
+// barrier (8192 x 5120 69.5 us, with one piece 78; 8192 x 8192 107, not 110; fp32 81
 // us for 4096 x 5003, with one piece 75).
 template <typename T, typename F>
 auto with_forward_shape(int64_t cols, F&& f) {
@@ -370,7 +418,8 @@ void forward(const LayerNormArgs& a, hipStream_t s) {
     return;
   }
   with_forward_shape<T>(a.cols, [&](auto nt, auto v) {
-    hipLaunchKernelGGL((layernorm_kernel<T, nt, v, RES>), grid, dim3(nt), 0, s, a);
+    if (a.gain_f32) hipLaunchKernelGGL((layernorm_kernel<T, float, nt, v, RES>), grid, dim3(nt), 0, s, a);
+    else hipLaunchKernelGGL((layernorm_kernel<T, uint16_t, nt, v, RES>), grid, dim3(nt), 0, s, a);
   });
 }
 
