@@ -52,6 +52,23 @@ __device__ __forceinline__ void repack(Vec8<uint16_t> (&h)[V]) {
 template <int V>
 __device__ __forceinline__ void repack(Vec8<float> (&)[V]) {}
 
+// Waits for a vector's, or a value's, loads here.
+__device__ __forceinline__ void arrived(float& x) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(x));
+#endif
+}
+__device__ __forceinline__ void arrived(Vec8<uint16_t>& v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(v.u));
+#endif
+}
+__device__ __forceinline__ void arrived(Vec8<float>& v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(v.u[0]), "+v"(v.u[1]));
+#endif
+}
+
 // The row's moments in every thread: piece i of V of the thread's 8 elements
 // are columns (threadIdx.x + i * NT) * 8 and on, zeros past the row's end.
 // `red`: two of block_sum's.
@@ -297,6 +314,15 @@ __global__ __launch_bounds__(NT) void layernorm_backward_kernel(LayerNormBwdArgs
       }
       Vec8<T> out;
       out.set(o);
+      if constexpr (V == 1) {
+        // (the next row has to be there before this one is stored: the loop would wait
+        // for the store with it)
+        arrived(next.dy[0]);
+        arrived(next.h[0]);
+        if constexpr (DRES) arrived(next.dres[0]);
+        arrived(next.mean);
+        arrived(next.rstd);
+      }
       out.template store<true>(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.cols - c);
     }
   }
