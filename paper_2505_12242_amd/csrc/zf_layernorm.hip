@@ -240,8 +240,10 @@ __device__ __forceinline__ float2 block_sum2(float x, float y, float2 (&red)[NT 
 
 // A block takes rows one after the other, the next one's loads in flight where a
 // thread has one piece, and keeps its columns' sums for both gradients in registers.
-// 8192 x 5120 bf16 with a residual: 336 MB in 56 us, 6.0 TB/s, 0.89 of a copy's rate, of
-// which 4 join the partial sums.  GRADS: the gain's and the bias's partial sums are kept (the bias's
+// 8192 x 5120 bf16 with a residual: 336 MB in 74 us, of which 5 join the partial sums, 4.9
+// TB/s in the first kernel, bound by HBM through few loads in flight (the sums'
+// registers leave a CU one block); 56 us where the operands are those of the call
+// before, partly in the cache.  GRADS: the gain's and the bias's partial sums are kept (the bias's
 // behind all blocks' of the gain).
 template <typename T, int NT, int V, bool DRES, bool GRADS>
 __global__ __launch_bounds__(NT) void layernorm_backward_kernel(LayerNormBwdArgs a) {
@@ -412,8 +414,8 @@ int backward_threads(int64_t cols) {
   return with_shape(cols, [](auto nt, auto) { return static_cast<int>(nt); });
 }
 // Blocks of the backward kernel, and partial sums of either gradient: what the chip
-// holds at once, two rows each at least (8192 x 5120 56.3 us, with twice the blocks
-// 62.8: two rounds of them, and twice the sums).
+// holds at once, two rows each at least (8192 x 5120, operands in turn, 74 us, with twice
+// the blocks 79: two rounds of them, and twice the sums).
 int64_t backward_blocks(int64_t rows, int64_t cols) {
   const int64_t held = 256 * std::min(4, 1024 / backward_threads(cols));
   const int64_t each = std::max<int64_t>(2, (rows + held - 1) / held);
