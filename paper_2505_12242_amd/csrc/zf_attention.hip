@@ -222,6 +222,9 @@ __device__ __forceinline__ float finish_row(const AttentionArgs& a, const Sequen
   return any ? 1.0f / sum : 0.0f;
 }
 
+// The most pieces of a sequence's keys, of either form: the join holds one a lane.
+constexpr int kMaxPieces = 64;
+
 // Keys of a piece of a sequence of lk keys, and how many pieces it has.
 __device__ __forceinline__ int32_t piece_of(const AttentionArgs& a, int32_t lk) {
   return max(a.piece, ((lk + a.splits - 1) / a.splits + 127) / 128 * 128);
@@ -414,12 +417,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void attention_few_kernel(Attent
 }
 
 // The pieces' results of one token and head joined by W waves: weights exp(lse of the
-// piece - lse of all) (a piece a lane, at most 64); wave w adds pieces w, w + W, ...
+// piece - lse of all) (a piece a lane, at most kMaxPieces); wave w adds pieces w, w + W, ...
 // in order, and the waves' sums are added in order.  W 4 where there are many pieces, 1
 // where many rows (512 tokens x 32 heads in 4 pieces: the whole call 58 us, with 4
 // waves 75).
 template <int W>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
+  static_assert(kMaxPieces <= 64, "a piece a lane");
   __shared__ float sums[W > 1 ? W - 1 : 1][128];
   const int lane = threadIdx.x & 63, index = uniform_i32(threadIdx.x >> 6);
   const int wave = W == 1 ? 0 : index;
@@ -484,6 +488,10 @@ int64_t row_tiles(const AttentionArgs& a, int lg) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+int32_t pieces_within(int64_t splits) {
+  return static_cast<int32_t>(std::min<int64_t>(kMaxPieces, std::max<int64_t>(1, splits)));
+}
+
 // How a call is done.  Up to 8 rows a sequence (on average: the lengths are on the
 // device): by sequences and pieces of keys (48 tokens of 8 rows over 1 to 8000 keys 153
 // us, by tiles 194; 8 tokens x 32 key heads over 4096 keys 93, not 98; with 16 rows, 16
@@ -505,12 +513,10 @@ Form form_of(const AttentionArgs& a) {
     const int64_t piece = 128 * std::min<int64_t>(8, std::max<int64_t>(1, a.tokens_k * a.kv_heads / (256 * 128)));
     const int64_t splits = std::min(ceil_div(a.tokens_k, piece),
                                     std::max(ceil_div(a.tokens_k, piece * a.sequences), 2048 / blocks));
-    return Form{true, static_cast<int32_t>(std::min<int64_t>(64, std::max<int64_t>(1, splits))),
-                static_cast<int32_t>(piece)};
+    return Form{true, pieces_within(splits), static_cast<int32_t>(piece)};
   }
   const int64_t blocks = row_tiles(a, kRowsLg) * a.kv_heads;
-  const int64_t splits = std::max<int64_t>(1, std::min(512 / blocks, most / 2));
-  return Form{false, static_cast<int32_t>(splits), 256};
+  return Form{false, pieces_within(std::min(512 / blocks, most / 2)), 256};
 }
 
 template <int DP>
