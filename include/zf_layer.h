@@ -273,7 +273,8 @@ size_t zf_attention_forward_workspace_bytes(const zf_attention* a);
 
 /* For every query and head, over the keys j that it sees, s[j] = scale * q . k[j]:
  *   lse = log sum exp(s);   out = round(sum of exp(s[j] - lse) * v[j])
- * A query that sees no key gets zeros and lse = -infinity.  Scores, sums and
+ * A key whose score is -infinity has weight 0.  A query that sees no key, or
+ * none of another score, gets zeros and lse = -infinity.  Scores, sums and
  * statistics are fp32, the weights of v are rounded to bf16.  out depends on
  * no key that its query does not see.  lse: fp32 [heads][tokens_q], may be
  * NULL.  Rows of out and lse in no sequence are not written.  ws:

@@ -266,14 +266,17 @@ __device__ __forceinline__ void wait_own_dma() {
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Loads tiles of N keys of k and v: the wave's part of each (`waves` of them load
-// together), rows past the last key repeating it, units past the head's width
-// the last one (the other operand is zero there, or the result not stored).  NT:
-// each is read by one block (nontemporal).
+// together), rows past the last key repeating it, units past the head's width as
+// zeros: their offsets lie beyond the resource, and such loads write zeros.  (The
+// other operand is zero there, but 0 x infinity, were they copies of other units,
+// is not: a key whose score is -infinity would have none.)  NT: each is read by one
+// block (nontemporal).
 template <int DP, int N, int WAVES, bool NT = false>
 struct KeyLoader {
   typedef Heads<DP> H;
   static constexpr int kLoads = N / H::kPer / WAVES;  // of a wave, of either
   static constexpr int kTile = N * H::kPitch;
+  static constexpr uint32_t kBeyond = 0x80000000u;  // (a tile's offsets are below half of it)
   const uint16_t *k, *v;
   int64_t ldk, ldv;
   uint32_t at[2][kLoads], unit[kLoads];
@@ -290,7 +293,8 @@ struct KeyLoader {
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       row[n] = (wave * kLoads + n) * H::kPer + lane / H::kUnits;
-      unit[n] = 16 * min((lane % H::kUnits) ^ H::swizzle(row[n]), a.dim / 8 - 1);
+      const int u = (lane % H::kUnits) ^ H::swizzle(row[n]);
+      unit[n] = u < a.dim / 8 ? 16 * u : kBeyond;
       at[0][n] = offset(row[n], ldk) + unit[n];
       at[1][n] = offset(row[n], ldv) + unit[n];
     }
@@ -302,7 +306,7 @@ struct KeyLoader {
   // `lds`.  kb < keys.
   template <bool K, bool V>
   __device__ __forceinline__ void load(int32_t kb, uint32_t lds, int wave) const {
-    const rsrc_t rk = make_rsrc(k + kb * ldk, -1), rv = make_rsrc(v + kb * ldv, -1);
+    const rsrc_t rk = make_rsrc(k + kb * ldk, kBeyond), rv = make_rsrc(v + kb * ldv, kBeyond);
     lds += wave * kLoads * 1024;
     const uint32_t to_v = K ? lds + kTile : lds;
     if (kb + N <= keys) {

@@ -1,7 +1,11 @@
 """zf_attention_forward and zf_attention_backward against 64 bits, in the forms
-that sizes select: many pieces of few rows' keys."""
-import pytest
+that sizes select: many pieces of few rows' keys; keys that are not finite."""
+import math
 
+import pytest
+import torch
+
+from _attention import F64, forward, seen
 from test_gpu_layer_attention import Case, check_backward, check_forward
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +38,41 @@ def test_gradients_of_few_rows_over_many_keys():
     check_forward(c, *got)
     check_backward(c, *got, zf.attention_backward(c.gdo, c.gq, c.gk, c.gv, *got, c.seq_q, c.seq_k,
                                                   c.causal, c.scale))
+
+
+@pytest.mark.parametrize("lens,heads,kv", [([(130, 200), (7, 90)], 4, 2), ([(1, 300), (2, 77)], 2, 1),
+                                           ([(40, 1000)], 4, 1)])
+@pytest.mark.parametrize("dim", [8, 40, 72, 80, 104, 120, 128])
+@pytest.mark.parametrize("value", [-math.inf, math.inf, math.nan])
+def test_an_infinite_element_of_a_key(lens, heads, kv, dim, value):
+    """In the last unit of 16 bytes, behind which a width's padding begins: a score of
+    minus infinity hides the key, others are NaN in the end."""
+    for e in (dim - 1, dim - 8):
+        c = Case(lens, heads, kv, dim)
+        at = lens[0][1] // 2
+        c.gk[c.ks[0] + at, 0, e] = value
+        out, lse = c.run()
+        k = c.k[c.ks[0]:c.ks[1], 0].clone()
+        rows = slice(c.qs[0], c.qs[1])
+        for h in range(heads // kv):
+            mask = seen(*lens[0], True)
+            s = c.q[rows, h, e].float() * value
+            bad = mask[:, at] & (s != -math.inf)
+            mask[:, at] = False
+            o, l, tol, ltol = forward(c.q[rows, h], k, c.v[c.ks[0]:c.ks[1], 0], mask, c.scale)
+            got, gl = out[rows, h].cpu().to(F64), lse[h, rows].cpu().to(F64)
+            assert not torch.isfinite(got[bad]).any() and not torch.isfinite(gl[bad]).any()
+            assert ((got - o).abs() <= tol)[~bad].all(), (h, e)
+            assert ((gl - l).abs() <= ltol)[~bad].all()
+
+
+@pytest.mark.parametrize("lens,heads,kv", [([(130, 200)], 4, 2), ([(1, 300)], 2, 1)])
+@pytest.mark.parametrize("dim", [72, 128])
+def test_scores_of_minus_infinity_alone(lens, heads, kv, dim):
+    """A query whose scores all are has zeros, as if it saw no key."""
+    c = Case(lens, heads, kv, dim)
+    c.gq[..., dim - 1] = 1.0
+    c.gk[c.ks[0]:c.ks[1], :, dim - 1] = -math.inf
+    out, lse = c.run()
+    rows = slice(c.qs[0], c.qs[1])
+    assert (out[rows] == 0).all() and (lse[:, rows] == -math.inf).all()
