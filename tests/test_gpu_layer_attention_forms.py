@@ -1,5 +1,6 @@
 """zf_attention_forward and zf_attention_backward against 64 bits, in the forms
-that sizes select: many pieces of few rows' keys; keys that are not finite."""
+that sizes select: many pieces of few rows' keys; blocks of the gradients of k
+and v; a prompt among single tokens; keys that are not finite."""
 import math
 
 import pytest
@@ -38,6 +39,40 @@ def test_gradients_of_few_rows_over_many_keys():
     check_forward(c, *got)
     check_backward(c, *got, zf.attention_backward(c.gdo, c.gq, c.gk, c.gv, *got, c.seq_q, c.seq_k,
                                                   c.causal, c.scale))
+
+
+RAGGED = [(40, 60), (33, 20), (130, 140), (1, 129), (17, 17)] * 9
+# (128 keys a block: (keys / 128 + sequences) * kv blocks, 448 and more)
+GRADIENTS = [
+    # 1120 blocks: one group of waves
+    dict(lens=RAGGED, heads=48, kv=16, dim=128),
+    dict(lens=RAGGED, heads=48, kv=16, dim=80),
+    dict(lens=RAGGED, heads=32, kv=16, dim=40, layout="heads"),
+    dict(lens=RAGGED, heads=32, kv=16, dim=96, causal=False),
+    # 576: two groups where causal
+    dict(lens=[(150, 200), (260, 260), (70, 190)] * 3, heads=48, kv=24, dim=128),
+    dict(lens=[(150, 200), (260, 260), (70, 190)] * 3, heads=48, kv=24, dim=88, layout="wide"),
+    # fewer: 32 keys a block, eight waves where walks are long
+    dict(lens=[(420, 300), (17, 40)], heads=8, kv=1, dim=128),
+    dict(lens=[(420, 300), (17, 40)], heads=8, kv=1, dim=128, causal=False),
+    dict(lens=[(420, 300), (17, 40)], heads=8, kv=1, dim=64),
+]
+
+
+@pytest.mark.parametrize("kw", GRADIENTS, ids=lambda kw: f"{len(kw['lens'])}x{kw['heads']}x{kw['dim']}")
+def test_gradients_by_form(kw):
+    c = Case(**kw)
+    got = c.run()
+    check_forward(c, *got)
+    check_backward(c, *got, zf.attention_backward(c.gdo, c.gq, c.gk, c.gv, *got, c.seq_q, c.seq_k,
+                                                  c.causal, c.scale))
+
+
+@pytest.mark.parametrize("heads,kv,dim,causal", [(2, 2, 128, True), (1, 1, 64, False), (2, 1, 80, True)])
+def test_a_prompt_among_single_tokens(heads, kv, dim, causal):
+    """Up to 8 rows a sequence on average: a block walks the prompt's rows, 32 at a time."""
+    c = Case([(1, 50)] * 31 + [(310 * kv // heads, 600)] + [(1, 7)] * 40, heads, kv, dim, causal)
+    check_forward(c, *c.run())
 
 
 @pytest.mark.parametrize("lens,heads,kv", [([(130, 200), (7, 90)], 4, 2), ([(1, 300), (2, 77)], 2, 1),
