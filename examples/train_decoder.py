@@ -34,6 +34,14 @@ BF16, F32 = torch.bfloat16, torch.float32
 QKV, OUT, UP, DOWN, HEAD = range(5)
 
 
+def embedding_gradient(tokens, dx, vocab):
+    """[vocab, dim] in fp32: the rows of dx summed by token, in their order (index_add_'s
+    atomics would add them in another order on every run)."""
+    order = tokens.argsort(stable=True)
+    starts = torch.searchsorted(tokens[order], torch.arange(vocab + 1, device=tokens.device))
+    return torch.segment_reduce(dx[order].float(), "sum", offsets=starts, initial=0)
+
+
 class Decoder:
     def __init__(self, vocab=64, dim=256, heads=4, kv=2, width=64, ffn=512, lr=2e-3, seed=0,
                  device="cuda"):
@@ -134,7 +142,7 @@ class Decoder:
         weight(QKV, columns(n1.y), g.qt)
         dx, _, _ = zf.layernorm_backward(zf.matmul_fp8(g.q, wt[QKV]), x, norms[0], n1.mean, n1.rstd,
                                          dresidual=dh1, dgain=dnorms[0], dbias=dnorms[1])
-        self.grads[10].zero_().index_add_(0, tokens, dx.float())
+        self.grads[10].copy_(embedding_gradient(tokens, dx, len(table)))
         # update: the linear weights by channel, the rest in one launch, clipped
         self.steps += 1
         self.runner.step()
