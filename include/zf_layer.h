@@ -280,7 +280,11 @@ size_t zf_attention_forward_workspace_bytes(const zf_attention* a);
  * NULL.  Rows of out and lse in no sequence are not written.  ws:
  * zf_attention_forward_workspace_bytes(a) bytes, 16-byte aligned (may be NULL
  * if that is 0), contents overwritten.  The keys' order of addition depends on
- * the sizes of `a` and on the sequence's own lengths only. */
+ * the sizes of `a` and on the sequence's own lengths only.
+ * Where the sequences have up to 8 rows (queries times heads / kv_heads) on
+ * average, one block walks a sequence's rows: a long prompt among many single
+ * tokens is better given a call of its own (4096 tokens among 1024 single ones 6
+ * times, with 8 heads 16 times as fast). */
 zf_status zf_attention_forward(const zf_attention* a, const zf_heads* q, const zf_heads* k,
                                const zf_heads* v, const zf_heads* out, float* lse, void* ws,
                                size_t ws_bytes, zf_stream stream);

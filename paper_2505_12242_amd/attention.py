@@ -125,7 +125,9 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     int32, how many of a sequence's keys are used, for a cache with room.  They
     are read on the GPU: a captured call follows their contents.  With causal,
     a sequence's last query sees all of its keys, the one before one less, and
-    so on: a prompt, a chunk of one behind a cache, or a single token.
+    so on: a prompt, a chunk of one behind a cache, or a single token.  (Long prompts
+    among many single tokens are faster in a call of their own: how a call is divided
+    follows its sequences' average length.)
 
     out: bf16 as q; lse (want_lse, or given): fp32 [heads, tokens], for
     attention_backward.  New ones hold nothing where tokens belong to no

@@ -8,8 +8,11 @@
 // the weights are an operand of the second product where they stand.  One pass
 // with the running maximum and sum; the sums are scaled down only when the
 // maximum has grown by more than 2^8, so that most tiles leave them alone.
-// (The weights are rounded to bf16, whatever power of two the maximum lags by: the
-// rounding is relative.  The sum that divides them is of the unrounded ones.)
+// (The weights are rounded to bf16, as the instruction takes them, whatever power of two
+// the maximum lags by: the rounding is relative.  The sum that divides them is of the
+// unrounded ones.  Against 64 bits the result's relative error, 2-norm, is 2.0e-3 to
+// 2.2e-3 where its own rounding makes 1.6e-3; with a second operand for what the rounding
+// leaves it would be the latter, for half as many products again.)
 //
 // Bound by the matrix instructions and, between them, the exponentials: 16384
 // tokens x 32 heads of 128, causal, 2.2e12 operations in 2.08 ms, 1.06 PFLOP/s,
@@ -496,6 +499,9 @@ int32_t pieces_within(int64_t splits) {
 // device): by sequences and pieces of keys (48 tokens of 8 rows over 1 to 8000 keys 153
 // us, by tiles 194; 8 tokens x 32 key heads over 4096 keys 93, not 98; with 16 rows, 16
 // sequences x 8 key heads over 4096 keys, 55, by tiles 52.7; with 32 rows 61 and 54.4).
+// A block walks all rows of its sequence, 32 at a time, so that one long prompt among
+// many tokens sets the call's time (4096 tokens among 1024 single ones, 32 heads: 4.08 ms,
+// in two calls 0.70; 8 heads 3.55 and 0.22).
 // Else by tiles of 128 rows, and by pieces of keys as often as the 512 blocks that the
 // chip holds allow (512 tokens x 32 heads over 4096 keys 60 us, whole 76; 1024 x 32
 // heads, 288 blocks, 25, in 3 pieces 42).

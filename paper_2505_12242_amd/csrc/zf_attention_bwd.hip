@@ -9,6 +9,10 @@
 // gradient is summed across blocks: no atomics, no partial results in memory, and
 // the same bits on every run.  2 x 4096 tokens x 32 heads of 128, causal: 400 us and
 // 550, 1.0 PFLOP/s of these products either (the library's 8192^3 bf16 product 1.26).
+// P and dS are rounded to bf16, as the instruction takes them: against 64 bits the
+// gradients' relative error (2-norm) is 2.35e-3 where one rounding of the results makes
+// 1.66e-3.  With a second operand for what the rounding leaves it would be the latter,
+// for three more products.
 //
 // In either, the operand that a wave keeps (rows, or keys) stays in registers and
 // runs along the lanes of the scores; what is walked runs along their registers,
@@ -469,14 +473,20 @@ __global__ __launch_bounds__(64 * WK * WR, 2) void attention_dkv_kernel(Attentio
 }
 
 // Forms by the number of blocks of 128 keys (of 512 that the chip holds at once).
+// (All gradients of a call, causal, heads 128 wide where no width is said.)
 // Few: blocks of 32 keys, whose waves share the walk.  Of these eight waves a block
-// where all of them are on the chip at once, more or less, and long enough, else four
-// (11 sequences of 1 to 1003 x 4 key heads x 5: 85 us, with four 102; 4 x 1024 x 12
-// heads 54, with eight 81; 4096 x 8 key heads x 4 534 and 558; one group of waves and
-// 128 keys a block 214 us for the first).  Causal, up to two rounds: the first keys'
-// blocks would be the last to end, so two groups of waves share a walk (8192 x 8 key
-// heads 1940 us, one group 2400; whole 485, not 466).  Else one group, without the
-// second one's barriers (2 x 4096 x 32 heads 993, not 1046).
+// where walks are long and the blocks at most 512, else four.  A CU holds one block of
+// eight waves, or two of heads up to 64 wide, by LDS, and two of four waves: 512 are up
+// to two rounds of the chip, but the last block's walk is what counts (504 blocks, 11
+// sequences of 1 to 1003 x 4 key heads x 5, 80 wide: 88 us, with four waves 106; 257,
+// 8192 x 1 key head x 8: 930 and 1209; 312 with short walks, 2 x 600 x 8 heads: 46 and
+// 35; 784, 2 x 1536 x 8 key heads x 4: 203 and 185; 1032, 4096 x 8 key heads x 4: 550
+// and 529.  Over a single key head with very long walks eight would win beyond the limit
+// too: 513, 16384 x 8: 2881 and 3454.)  128 keys a block and one group of waves take 221
+// us for the first.  Causal, up to two rounds: the first keys' blocks would be the last
+// to end, so two groups of waves share a walk (8192 x 8 key heads x 4 1840 us, one group
+// 2335; not causal 3451 and 3416).  Else one group, without the second one's barriers (2
+// x 4096 x 32 heads 955, with two 1000).
 enum { kNarrow, kNarrowLong, kTwoGroups, kWide };
 constexpr int64_t kFewBlocks = 448, kTwoRounds = 1024, kLongRows = 1536;
 int32_t form_of(const AttentionBwdArgs& a) {
@@ -491,9 +501,10 @@ int32_t form_of(const AttentionBwdArgs& a) {
 
 int64_t row_tiles(const AttentionBwdArgs& a, int lg) { return (a.tokens_q * a.group >> lg) + a.sequences; }
 // dq by blocks of 32 rows where those of 128 are fewer than the CUs, and a walk's length is
-// what counts (both gradients, 132 blocks: 4096 tokens x 4 heads 110 us, with 128 rows
-// 172; 144: 1024 x 16 heads 42, 56; 288: 1024 x 32 heads 72.7, 73.8; 272: 2 x 512 x 8 key
-// heads x 4 57.8, 53.9; 620: the first of the above 92, 85).
+// what counts (all gradients, 132 blocks: 4096 tokens x 4 heads 113 us, with 128 rows
+// 174; 144: 1024 x 16 heads 42, 56; 260: 2 x 2048 x 2 key heads x 4 143, 162; 288: 1024 x
+// 32 heads 72.7, 73.8; 272: 2 x 512 x 8 key heads x 4 57.8, 53.9; 620: the first of the
+// above 96, 91).
 bool dq_narrow(const AttentionBwdArgs& a) { return row_tiles(a, kLg) * a.kv_heads <= 256; }
 
 template <int DP, int WK, int WR>
